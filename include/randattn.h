@@ -36,7 +36,8 @@
  *   and the device state may disagree, and the cache should be destroyed.
  *   Nothing throws across the ABI.
  * - head_dim must be 128; dtype f32 or bf16 (keys, values, queries and
- *   outputs all in that dtype); positions are int32.
+ *   outputs all in that dtype) or e4m3 (rows held in 8 bits, every array
+ *   that a call takes or gives in bf16: see ra_dtype); positions are int32.
  *
  * Eviction rule (what the kernels compute; the CPU oracle restates it)
  * -----------------------------------------------------------------
@@ -76,7 +77,24 @@ typedef enum {
   RA_ERR_STATE = -6         /* call out of protocol order for this state */
 } ra_status;
 
-typedef enum { RA_F32 = 0, RA_BF16 = 1 } ra_dtype;
+typedef enum {
+  RA_F32 = 0,
+  RA_BF16 = 1,
+  RA_E4M3 = 2  /* a cache in 8 bits: rows are quantised as they are written
+                  (prompts, ra_write_rows, the step's new pair) and read back
+                  as bf16; queries, new pairs and outputs are bf16.  A row is
+                  128 OCP E4M3 codes and a scale 2^s: with amax the largest
+                  |x_c| = f * 2^e of the row (1 <= f < 2), s = e - 8 where
+                  f <= 1.75, else e - 7, at least -126, and code_c = E4M3(x_c /
+                  2^s) to nearest even (at most 448; at most 240 where s = 120,
+                  so that every value is a bf16 number).  An infinity counts as
+                  the largest bf16 number; a NaN stays one and does not count
+                  in amax.  What is read back is exactly what the codes stand
+                  for, writing it again gives the same values, and attention
+                  attends to these values, the new pair's included.  Not with
+                  RA_LAYOUT_HOLE_FILL, ra_window_select or ra_scored_evict
+                  (RA_ERR_UNSUPPORTED). */
+} ra_dtype;
 
 typedef enum {
   RA_BUDGET_EVICTABLE = 0,  /* budget_k counts kept non-prompt, non-buffer rows */
@@ -219,6 +237,11 @@ int64_t ra_seq_rows(const ra_config* cfg, int32_t prompt_len);
 int64_t ra_required_slots(const ra_config* cfg, const int32_t* host_prompt_lens,
                           int32_t n_seqs);
 
+/* Bytes of each of the K and V pools of a cache of pool_rows rows: head_dim
+ * elements of the dtype per row; for RA_E4M3 the codes, one byte each, of all
+ * rows and then a scale byte per row, 129 bytes in all.  0 on a bad config. */
+size_t ra_pool_bytes(const ra_config* cfg, int64_t pool_rows);
+
 /* Bytes of the persistent device metadata buffer: per-slot state; in the
  * paged layout the block tables, max_seqs * ceil((max_prompt_len + k_keep +
  * recent_r + evict_every) / page_rows) int32; in the bf16 chronological
@@ -236,7 +259,7 @@ size_t ra_workspace_bytes(const ra_config* cfg);
 /* ---- lifetime ----------------------------------------------------------- */
 
 /* Create a cache over caller-owned device buffers:
- *   k_pool, v_pool: pool_rows * head_dim elements of cfg->dtype each;
+ *   k_pool, v_pool: ra_pool_bytes(cfg, pool_rows) bytes each;
  *   pos_pool:       pool_rows int32;
  *   meta:           ra_meta_bytes(cfg) bytes (zeroed here on `stream`).
  * pool_rows is a multiple of 32 (of L * Hkv * page_rows, one page group, in
@@ -377,6 +400,59 @@ ra_status ra_graph_mode(ra_cache* cache, int32_t on, void* stream);
  * Attention's (or the policy's). */
 ra_status ra_evict_now(ra_cache* cache, int32_t seq, void* stream);
 
+/* ---- block-sparse decode attention ---------------------------------------------- */
+
+/* A decode step may attend to part of a head's rows, chosen for each KV head by
+ * its queries (bf16 and e4m3 caches of the chronological and paged layouts).
+ * Of the `len` rows that a head holds before the step's append, blocks of 32
+ * consecutive rows that end at or below row len - recent_rows are candidates; every
+ * later row and the new pair are always attended.  Where a head has more than
+ * n_blocks candidates, the n_blocks of highest score are attended, the lowest block
+ * first among equal scores; otherwise all of them, and the result is that of
+ * ra_decode_attention.
+ * A block's score bounds the products of its keys with the head's queries from
+ * above, in 8 bits: with hi_c and lo_c the largest and smallest value of channel c
+ * over its rows and 2^t the power of two that brings max_c max(|hi_c|, |lo_c|) into
+ * (63.5, 127], H_c = ceil(hi_c / 2^t) and L_c = floor(lo_c / 2^t); with 2^u the same
+ * for a query row, Q_c = q_c / 2^u rounded to nearest even;
+ *   score = max over the G query heads of 2^(t+u) * sum_c (Q_c > 0 ? Q_c H_c : Q_c L_c)
+ * (t and u within [-60, 50], the integers clamped to +-127; a NaN counts as 0, an
+ * infinity as the largest bf16 number).  The sums are exact, so the choice is the
+ * same on every run.  A step reads 257 bytes per candidate block and the rows of the
+ * attended ones.
+ *
+ * The bounds live in a buffer of the caller's, attached to the cache.  They are
+ * computed when a step first needs them and again where rows have changed since (an
+ * event, ra_write_rows, a fast forward, a new sequence in the slot), from the cached
+ * keys, on the step's stream.  While a buffer is attached events do not defer their
+ * row moves (ra_end_step). */
+
+/* Bytes of the bounds buffer for a pool of pool_rows rows (257 per 32 rows); 0 on a
+ * bad config or one whose dtype or layout has no sparse steps. */
+size_t ra_sparse_bytes(const ra_config* cfg, int64_t pool_rows);
+
+/* Bytes of the workspace of a sparse step choosing n_blocks blocks per head (any
+ * smaller n_blocks may use it too): the lists and the split partials.  0 as above or
+ * if n_blocks < 0. */
+size_t ra_sparse_workspace_bytes(const ra_config* cfg, int32_t n_blocks);
+
+/* Attach a bounds buffer (ra_sparse_bytes bytes, 16-byte aligned; contents need not
+ * be set), or detach with NULL.  It is read and written by sparse steps until it is
+ * replaced, detached or the cache destroyed.  RA_ERR_STATE inside an open step or in
+ * graph mode. */
+ra_status ra_sparse_attach(ra_cache* cache, void* dev_bounds, size_t bounds_bytes,
+                           void* stream);
+
+/* ra_decode_attention over the chosen blocks (see above): the same append, arrays,
+ * step protocol and errors, one call per layer and step in its place (the layers of
+ * a step may mix both).  RA_ERR_STATE if no bounds are attached or in graph mode;
+ * RA_ERR_UNSUPPORTED for fp32, the hole-fill layout, or a head with more than 16384
+ * candidates where that is more than n_blocks. */
+ra_status ra_sparse_attention(ra_cache* cache, int32_t layer, int32_t n_blocks,
+                              int32_t recent_rows, const void* q, const void* k_new,
+                              const void* v_new, void* out, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
 /* ---- state transfer and audit --------------------------------------------- */
 
 /* Advance every active sequence by n_steps decode steps touching positions
@@ -411,6 +487,13 @@ ra_status ra_seq_fast_forward(ra_cache* cache, int32_t seq, int32_t n_steps,
  * nothing copied, if out_elems is smaller; NULL allowed when len is 0). */
 ra_status ra_export_positions(ra_cache* cache, int32_t seq, int32_t* dev_out,
                               int64_t out_elems, void* stream);
+
+/* Copy slot `seq`'s cached rows, every head of every layer, to row-major device
+ * arrays [L][Hkv][len][d], the layout ra_write_rows takes (RA_ERR_CAPACITY,
+ * nothing copied, if out_elems, the elements of each array, is smaller).  Either
+ * array may be NULL. */
+ra_status ra_export_rows(ra_cache* cache, int32_t seq, void* dev_k_out, void* dev_v_out,
+                         int64_t out_elems, void* stream);
 
 /* Overwrite slot `seq`'s cached rows from row-major device arrays
  * [L][Hkv][len][d] (row j belongs to the j-th cached position, the order of

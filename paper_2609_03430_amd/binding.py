@@ -27,7 +27,7 @@ RA_ERR_BUDGET = -3
 RA_ERR_UNSUPPORTED = -4
 RA_ERR_HIP = -5
 RA_ERR_STATE = -6
-RA_F32, RA_BF16 = 0, 1
+RA_F32, RA_BF16, RA_E4M3 = 0, 1, 2
 RA_BUDGET_EVICTABLE, RA_BUDGET_TOTAL = 0, 1
 RA_LAYOUT_CHRONOLOGICAL, RA_LAYOUT_HOLE_FILL, RA_LAYOUT_PAGED = 0, 1, 2
 RA_POLICY_RANDOM, RA_POLICY_SHARED, RA_POLICY_BLOCK, RA_POLICY_RECENCY = 0, 1, 2, 3
@@ -38,7 +38,7 @@ RA_NOALLOC_SCRATCH_BYTES = 8 << 20
 # Every entry point declared in include/randattn.h.
 EXPORTS = (
     "ra_config_check", "ra_region_rows", "ra_seq_rows", "ra_required_slots",
-    "ra_meta_bytes",
+    "ra_pool_bytes", "ra_meta_bytes",
     "ra_workspace_bytes", "ra_cache_create", "ra_cache_destroy",
     "ra_pool_info", "ra_seq_begin", "ra_seq_end", "ra_get_seq_info", "ra_decode_attention",
     "ra_decode_attention_noalloc",
@@ -47,6 +47,8 @@ EXPORTS = (
     "ra_write_rows", "ra_read_rows", "ra_read_positions", "ra_status_string",
     "ra_last_hip_error", "ra_attention_plan", "ra_window_select",
     "ra_scored_scratch_bytes", "ra_scored_evict",
+    "ra_export_rows", "ra_sparse_bytes", "ra_sparse_workspace_bytes", "ra_sparse_attach",
+    "ra_sparse_attention",
 )
 
 
@@ -98,6 +100,7 @@ _SIGS = {
     "ra_region_rows": (_I64, [_CFG, _I32]),
     "ra_seq_rows": (_I64, [_CFG, _I32]),
     "ra_required_slots": (_I64, [_CFG, ctypes.POINTER(ctypes.c_int32), _I32]),
+    "ra_pool_bytes": (_SZ, [_CFG, _I64]),
     "ra_meta_bytes": (_SZ, [_CFG]),
     "ra_workspace_bytes": (_SZ, [_CFG]),
     "ra_cache_create": (_I32, [_CFG, _P, _P, _P, _I64, _P, _SZ, _P,
@@ -126,6 +129,11 @@ _SIGS = {
     "ra_window_select": (_I32, [_P, _I32, _I32, _P, _P, _I32, _P, _P]),
     "ra_scored_scratch_bytes": (ctypes.c_size_t, [_P, _I32]),
     "ra_scored_evict": (_I32, [_P, _I32, _I32, _P, _P, _P, ctypes.c_size_t, _P]),
+    "ra_export_rows": (_I32, [_P, _I32, _P, _P, _I64, _P]),
+    "ra_sparse_bytes": (_SZ, [_CFG, _I64]),
+    "ra_sparse_workspace_bytes": (_SZ, [_CFG, _I32]),
+    "ra_sparse_attach": (_I32, [_P, _P, _SZ, _P]),
+    "ra_sparse_attention": (_I32, [_P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _SZ, _P]),
 }
 
 _handle = None
@@ -171,7 +179,12 @@ def _cfg_of(handle):
 
 
 def _cache_dtype(cfg):
-    return torch.bfloat16 if cfg.dtype == RA_BF16 else torch.float32
+    """dtype of the rows, queries and outputs that calls take and give."""
+    return torch.float32 if cfg.dtype == RA_F32 else torch.bfloat16
+
+
+def _bytes(t):
+    return t.numel() * t.element_size()
 
 
 def _arg(t, where, name, dtype=None, numel=0):
@@ -250,6 +263,10 @@ def ra_required_slots(cfg, prompt_lens):
     return _lib().ra_required_slots(ctypes.byref(cfg), arr, len(prompt_lens))
 
 
+def ra_pool_bytes(cfg, pool_rows):
+    return _lib().ra_pool_bytes(ctypes.byref(cfg), int(pool_rows))
+
+
 def ra_meta_bytes(cfg):
     return _lib().ra_meta_bytes(ctypes.byref(cfg))
 
@@ -261,9 +278,12 @@ def ra_workspace_bytes(cfg):
 def ra_cache_create(cfg, k_pool, v_pool, pos_pool, pool_rows, meta, stream=None):
     where = "ra_cache_create"
     if ra_config_check(cfg) == RA_OK:
-        rows = int(pool_rows) * cfg.head_dim
-        _arg(k_pool, where, "k_pool", _cache_dtype(cfg), rows)
-        _arg(v_pool, where, "v_pool", _cache_dtype(cfg), rows)
+        if cfg.dtype == RA_E4M3:
+            pool, n = torch.uint8, ra_pool_bytes(cfg, pool_rows)
+        else:
+            pool, n = _cache_dtype(cfg), int(pool_rows) * cfg.head_dim
+        _arg(k_pool, where, "k_pool", pool, n)
+        _arg(v_pool, where, "v_pool", pool, n)
         _arg(pos_pool, where, "pos_pool", torch.int32, int(pool_rows))
         _arg(meta, where, "meta")
     out = ctypes.c_void_p()
@@ -403,6 +423,18 @@ def ra_read_rows(handle, seq, layer, kv_head, k_out=None, v_out=None,
            "ra_read_rows")
 
 
+def ra_export_rows(handle, seq, k_out=None, v_out=None, stream=None):
+    """Every head's cached rows: [L][Hkv][len][d] tensors."""
+    where, cfg = "ra_export_rows", _cfg_of(handle)
+    dt = None if cfg is None else _cache_dtype(cfg)
+    _arg(k_out, where, "k_out", dt)
+    _arg(v_out, where, "v_out", dt)
+    # (with no output there is nothing to hold the rows: any size will do)
+    n = min((t.numel() for t in (k_out, v_out) if t is not None), default=2 ** 62)
+    _check(_lib().ra_export_rows(handle, int(seq), _ptr(k_out), _ptr(v_out), n,
+                                 _stream(stream)), where)
+
+
 def ra_read_positions(handle, seq, layer, kv_head, cap, stream=None):
     """Synchronous; returns a numpy int32 array of the head's positions."""
     import numpy as np
@@ -447,6 +479,32 @@ def ra_scored_evict(handle, seq_lo, seq_hi, params, q_window, scratch, stream=No
                                   _stream(stream)), "ra_scored_evict")
 
 
+def ra_sparse_bytes(cfg, pool_rows):
+    return int(_lib().ra_sparse_bytes(ctypes.byref(cfg), int(pool_rows)))
+
+
+def ra_sparse_workspace_bytes(cfg, n_blocks):
+    return int(_lib().ra_sparse_workspace_bytes(ctypes.byref(cfg), int(n_blocks)))
+
+
+def ra_sparse_attach(handle, bounds, stream=None):
+    """Attach a bounds buffer (a device tensor kept alive by the caller), or detach
+    with None."""
+    _arg(bounds, "ra_sparse_attach", "bounds")
+    _check(_lib().ra_sparse_attach(handle, _ptr(bounds), 0 if bounds is None else _bytes(bounds),
+                                   _stream(stream)), "ra_sparse_attach")
+
+
+def ra_sparse_attention(handle, layer, n_blocks, recent_rows, q, k_new, v_new, out, workspace,
+                        stream=None):
+    _decode_args(handle, "ra_sparse_attention", q, k_new, v_new, out)
+    _arg(workspace, "ra_sparse_attention", "workspace")
+    _check(_lib().ra_sparse_attention(handle, int(layer), int(n_blocks), int(recent_rows),
+                                      _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                      _ptr(workspace), _bytes(workspace), _stream(stream)),
+           "ra_sparse_attention")
+
+
 def ra_attention_plan(handle):
     """(split_keys, max_splits, waves) of the next attention launch."""
     sk, ms, w = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int32(0)
@@ -467,13 +525,17 @@ class Cache:
         self.cfg = cfg
         self.device = torch.device(device)
         _check(ra_config_check(cfg), "ra_config_check")
-        self.dtype = torch.bfloat16 if cfg.dtype == RA_BF16 else torch.float32
+        self.dtype = _cache_dtype(cfg)
         pool_rows = int(pool_rows)
         pool_rows += (-pool_rows) % 32
         self.pool_rows = pool_rows
         d = cfg.head_dim
-        self.k_pool = torch.zeros(pool_rows, d, dtype=self.dtype, device=self.device)
-        self.v_pool = torch.zeros(pool_rows, d, dtype=self.dtype, device=self.device)
+        if cfg.dtype == RA_E4M3:
+            shape, dtype = (ra_pool_bytes(cfg, pool_rows),), torch.uint8
+        else:
+            shape, dtype = (pool_rows, d), self.dtype
+        self.k_pool = torch.zeros(shape, dtype=dtype, device=self.device)
+        self.v_pool = torch.zeros(shape, dtype=dtype, device=self.device)
         self.pos_pool = torch.zeros(pool_rows, dtype=torch.int32, device=self.device)
         self.meta = torch.zeros(ra_meta_bytes(cfg), dtype=torch.uint8, device=self.device)
         self.workspace = torch.empty(ra_workspace_bytes(cfg), dtype=torch.uint8,
@@ -498,3 +560,18 @@ class Cache:
 
     def decode_noalloc(self, layer, q, k_new, v_new, out, stream=None):
         ra_decode_attention_noalloc(self.handle, layer, q, k_new, v_new, out, stream)
+
+    def attach_sparse(self, n_blocks, stream=None):
+        """Bounds and workspace for sparse steps of up to n_blocks blocks per head."""
+        size = ra_sparse_bytes(self.cfg, self.pool_rows)
+        if size == 0:
+            raise RandAttnError(RA_ERR_UNSUPPORTED, "ra_sparse_bytes")
+        bounds = torch.empty(size, dtype=torch.uint8, device=self.device)
+        workspace = torch.empty(ra_sparse_workspace_bytes(self.cfg, n_blocks), dtype=torch.uint8,
+                                device=self.device)
+        ra_sparse_attach(self.handle, bounds, stream)
+        self.bounds, self.sparse_workspace = bounds, workspace
+
+    def decode_sparse(self, layer, n_blocks, recent_rows, q, k_new, v_new, out, stream=None):
+        ra_sparse_attention(self.handle, layer, n_blocks, recent_rows, q, k_new, v_new, out,
+                            self.sparse_workspace, stream)

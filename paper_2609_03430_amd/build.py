@@ -20,7 +20,8 @@ LIB = os.path.join(LIBDIR, "librandattn.so")
 OBJDIR = os.path.join(ROOT, "_build")
 # per-kernel register, scratch and LDS use reported by the compiler
 RESOURCES = os.path.join(OBJDIR, "kernel_resources.json")
-SOURCES = ["attention.hip", "evict.hip", "state.hip", "window_score.hip", "scored.hip", "api.cpp"]
+SOURCES = ["attention.hip", "attn_blocks.hip", "blocks.hip", "evict.hip", "state.hip",
+           "window_score.hip", "scored.hip", "api.cpp", "api_blocks.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -11,14 +11,20 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <map>
 #include <new>
 #include <vector>
 
-#include "randattn.h"
+#include "cache.h"
 #include "ra_internal.h"
+#include "randattn.h"
 
 using ra::SeqMeta;
+using ra::host::Plan;
+using ra::host::check_decode;
+using ra::host::flush_pending;
+using ra::host::grow_for_step;
+using ra::host::hip_fail;
+using ra::host::round_up;
 
 static_assert(RA_NOALLOC_SCRATCH_BYTES == ra::kNoAllocScratchBytes,
               "the header's no-alloc limit is the size of the device array");
@@ -27,19 +33,15 @@ namespace {
 
 std::atomic<int32_t> g_last_hip_error{0};
 
-ra_status hip_fail(hipError_t e) {
+}  // namespace
+
+ra_status ra::host::hip_fail(hipError_t e) {
   if (e == hipSuccess) return RA_OK;
   g_last_hip_error.store(static_cast<int32_t>(e));
   return RA_ERR_HIP;
 }
 
-#define RA_LAUNCH(expr)                         \
-  do {                                          \
-    const hipError_t e_ = (expr);               \
-    if (e_ != hipSuccess) return hip_fail(e_);  \
-  } while (0)
-
-int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+namespace {
 
 // The per-(sequence, layer, KV head) kernels (eviction, deferred moves,
 // external rounds' compaction) run one workgroup of up to 1,024 threads per
@@ -135,120 +137,7 @@ size_t drops_bytes(const ra_config& c) {
                                       256));
 }
 
-// Attention launch plan (plan_for): work items of split_keys keys, `waves`
-// wavefronts each; group_waves > 0: items of one wavefront, group_waves
-// consecutive items of a head to a workgroup.
-struct Plan {
-  int split_keys = 0, max_splits = 0, waves = 1, wide_regs = 0;
-  int group_waves = 0;
-  int short_runs = 0;   // every item is at most 64 keys: the latency build
-  // an event of every sequence may leave its row moves to the next step's
-  // attention, one workgroup per head (attn_bf16_move_kernel)
-  bool whole = false;
-  // partial slots per head that the no-alloc entry point's limit counts (at
-  // least the workgroups of a head)
-  int partials = 0;
-
-  int launch_waves() const { return group_waves ? group_waves : waves; }
-  int launch_keys() const { return group_waves ? group_waves * split_keys : split_keys; }
-  int launch_splits() const {
-    return group_waves ? (max_splits + group_waves - 1) / group_waves : max_splits;
-  }
-};
-
 }  // namespace
-
-struct ra_cache {
-  ra_config cfg{};
-  int G = 0;
-  size_t elem = 0;
-  void* kpool = nullptr;
-  void* vpool = nullptr;
-  int32_t* pos = nullptr;
-  int64_t pool_rows = 0;
-  SeqMeta* meta = nullptr;
-  std::vector<SeqMeta> mirror;           // host copy of the device metadata
-  std::map<int64_t, int64_t> free_rows;  // first-fit free list: base -> rows
-  std::vector<uint8_t> appended;         // layers appended in the open step
-  int n_appended = 0;
-  int slot_lo = 0, slot_hi = 0;          // range covering the active slots
-  // paged layout
-  ra::Paging pg{};                       // device tables and page geometry
-  int page_rows = 0;
-  int64_t n_groups = 0;                  // page groups in the pool
-  std::vector<int32_t> free_groups;      // stack: the next group is back()
-  std::vector<std::vector<int32_t>> groups;   // per slot: its table, in order
-  // deferred row moves (see ra_end_step)
-  int32_t* drops = nullptr;              // drop lists of the last events
-  int32_t* arrivals = nullptr;           // split arrival counters, event sync words
-  // graph mode (see ra_graph_mode): launches that depend on no host state
-  bool graph = false;
-  Plan graph_plan;
-  int graph_candidates = 0;              // bound on any event's candidate slots
-  void* scratch = nullptr;               // device address of the no-alloc partials
-
-  ra::Shape shape() const {
-    return ra::Shape{cfg.num_layers, cfg.num_q_heads, cfg.num_kv_heads, G,
-                     cfg.recent_r, cfg.evict_every, cfg.dtype, cfg.layout,
-                     cfg.policy, std::max(1, cfg.policy_block), pg};
-  }
-  bool is_paged() const { return cfg.layout == RA_LAYOUT_PAGED; }
-  bool any_pending() const {
-    for (int s = slot_lo; s < slot_hi; ++s)
-      if (mirror[s].active && mirror[s].due == ra::kDueMovePending) return true;
-    return false;
-  }
-  int64_t pages_for(int64_t rows) const { return (rows + page_rows - 1) / page_rows; }
-  // paged: whether `rows` rows fit the block table of one sequence (rows
-  // pile up past lp + k_keep + r + R only under the external policy)
-  bool fits_table(int64_t rows) const { return pages_for(rows) <= pg.pages_per_seq; }
-  // paged: page groups slot `s` must add to hold `rows` rows
-  int64_t groups_short(int s, int64_t rows) const {
-    return std::max<int64_t>(0, pages_for(rows) - static_cast<int64_t>(groups[s].size()));
-  }
-  // paged: take groups from the free list until slot `s` holds `rows` rows;
-  // the new table entries are appended to `out` (the caller checked that
-  // enough groups are free)
-  void grow(int s, int64_t rows, std::vector<ra::TableEntry>& out) {
-    while (static_cast<int64_t>(groups[s].size()) < pages_for(rows)) {
-      const int32_t g = free_groups.back();
-      free_groups.pop_back();
-      out.push_back(ra::TableEntry{s, static_cast<int32_t>(groups[s].size()), g});
-      groups[s].push_back(g);
-    }
-    mirror[s].cap = static_cast<int32_t>(groups[s].size()) * page_rows;
-  }
-  // paged: return the groups past the first pages_for(rows) to the free list
-  void shrink(int s, int64_t rows) {
-    while (static_cast<int64_t>(groups[s].size()) > pages_for(rows)) {
-      free_groups.push_back(groups[s].back());
-      groups[s].pop_back();
-    }
-    mirror[s].cap = static_cast<int32_t>(groups[s].size()) * page_rows;
-  }
-  bool step_open() const { return n_appended != 0; }
-  void update_range() {
-    slot_lo = 0;
-    slot_hi = 0;
-    bool any = false;
-    for (int s = 0; s < cfg.max_seqs; ++s) {
-      if (!mirror[s].active) continue;
-      if (!any) slot_lo = s;
-      slot_hi = s + 1;
-      any = true;
-    }
-  }
-  // slots the selection examines per head (see evict.hip)
-  int span(const SeqMeta& M) const {
-    return M.plan_len - M.prompt_len - (cfg.layout == RA_LAYOUT_HOLE_FILL ? 0 : cfg.recent_r);
-  }
-  int max_candidates_due() const {
-    int mx = 0;
-    for (int s = slot_lo; s < slot_hi; ++s)
-      if (mirror[s].active && mirror[s].due) mx = std::max(mx, span(mirror[s]));
-    return mx;
-  }
-};
 
 namespace {
 
@@ -382,11 +271,32 @@ int mid_plan(const ra_cache* c, Plan& p, int heads, int keys_max, int64_t keys_m
              ? 2 : 1;
 }
 
+}  // namespace
+
+// Attention over blocks of rows (attn_blocks.hip): `heads` heads of up to keys_max
+// attended rows.
+Plan ra::host::plan_blocks(const ra_cache* c, int64_t keys_max, int heads) {
+  Plan p;
+  p.waves = 4;
+  const int unit = 32 * p.waves;
+  const int64_t splits =
+      std::min<int64_t>(ra::kMaxSplits, heads >= 768 ? 1 : (512 + heads - 1) / heads);
+  int64_t sk = c->cfg.attn_split > 0 ? c->cfg.attn_split : (keys_max + splits - 1) / splits;
+  sk = std::max(sk, (keys_max + ra::kMaxSplits - 1) / ra::kMaxSplits);
+  p.split_keys = static_cast<int>(round_up(sk, unit));
+  p.max_splits = p.partials = static_cast<int>((keys_max + p.split_keys - 1) / p.split_keys);
+  p.whole = p.max_splits == 1;
+  return p;
+}
+
+namespace {
+
 // The plan for `n_active` sequences whose longest cache, the new row
 // included, has keys_max keys, and the mean one keys_mean.
 Plan plan_for(const ra_cache* c, int keys_max, int64_t keys_mean, int n_active) {
   const int heads = std::max(1, n_active * c->cfg.num_kv_heads);
   const bool bf16 = c->cfg.dtype == RA_BF16;
+  if (c->cfg.dtype == RA_E4M3) return ra::host::plan_blocks(c, keys_max, heads);
   Plan p;
   int splits = 1;
   bool halved = false;
@@ -448,9 +358,10 @@ Plan attention_plan(const ra_cache* c) {
   return plan_for(c, keys_max, keys / std::max(1, n_active), n_active);
 }
 
-// Host checks shared by both attention entry points; nothing is launched.
-ra_status check_decode(const ra_cache* c, int32_t layer, const void* q, const void* k_new,
-                       const void* v_new, const void* out) {
+}  // namespace
+
+ra_status ra::host::check_decode(const ra_cache* c, int32_t layer, const void* q,
+                                 const void* k_new, const void* v_new, const void* out) {
   if (!c || layer < 0 || layer >= c->cfg.num_layers || !q || !k_new || !v_new || !out)
     return RA_ERR_INVALID_ARG;
   if (c->appended[layer]) return RA_ERR_STATE;
@@ -470,10 +381,17 @@ ra_status check_decode(const ra_cache* c, int32_t layer, const void* q, const vo
   return RA_OK;
 }
 
-// Moves the key/value rows of every sequence whose last event deferred them
-// (their positions are already compacted); a call that reads or writes rows,
-// or plans another event, runs this first.
-ra_status flush_pending(ra_cache* c, hipStream_t s) {
+ra_status ra::host::grow_for_step(ra_cache* c, hipStream_t s) {
+  if (!c->is_paged()) return RA_OK;
+  std::vector<ra::TableEntry> te;
+  for (int i = c->slot_lo; i < c->slot_hi; ++i)
+    if (c->mirror[i].active) c->grow(i, c->mirror[i].len + 1, te);
+  if (!te.empty())
+    RA_LAUNCH(ra::launch_table_set(c->shape(), te.data(), static_cast<int>(te.size()), s));
+  return RA_OK;
+}
+
+ra_status ra::host::flush_pending(ra_cache* c, hipStream_t s) {
   if (!c->any_pending()) return RA_OK;
   RA_LAUNCH(by_slot_chunks(c->cfg, c->slot_lo, c->slot_hi, [&](int lo, int hi) {
     return ra::launch_flush_pending(c->shape(), c->meta, c->kpool, c->vpool, c->drops,
@@ -483,6 +401,8 @@ ra_status flush_pending(ra_cache* c, hipStream_t s) {
     if (c->mirror[i].due == ra::kDueMovePending) c->mirror[i].due = 0;
   return RA_OK;
 }
+
+namespace {
 
 // Rows that the 256 MB last-level cache still holds at an event, beside the step's
 // inputs and outputs.
@@ -520,17 +440,8 @@ hipError_t launch_event(ra_cache* c, int lo, int hi, int candidates, bool deferr
 ra_status launch_decode(ra_cache* c, int32_t layer, const void* q, const void* k_new,
                         const void* v_new, void* out, const Plan& plan, float* ws_o,
                         float* ws_ml, int split_stride, hipStream_t stream) {
-  if (c->is_paged()) {
-    // pages for the rows this step appends (the first layer of the step)
-    std::vector<ra::TableEntry> te;
-    for (int s = c->slot_lo; s < c->slot_hi; ++s)
-      if (c->mirror[s].active) c->grow(s, c->mirror[s].len + 1, te);
-    if (!te.empty()) {
-      const hipError_t e = ra::launch_table_set(c->shape(), te.data(),
-                                                static_cast<int>(te.size()), stream);
-      if (e != hipSuccess) return hip_fail(e);
-    }
-  }
+  const ra_status grown = grow_for_step(c, stream);
+  if (grown != RA_OK) return grown;
   // rows of deferred events move in this step's attention where the plan
   // allows one workgroup per head; otherwise they move first, on their own
   bool move = false;
@@ -607,7 +518,7 @@ ra_status ra_config_check(const ra_config* c) {
       c->recent_r < 0 || c->evict_every < 1 || c->max_seqs < 1 ||
       c->max_seqs > 65536 || c->attn_split < 0 || c->attn_split % 32 != 0 ||
       (c->budget_mode != RA_BUDGET_EVICTABLE && c->budget_mode != RA_BUDGET_TOTAL) ||
-      (c->dtype != RA_F32 && c->dtype != RA_BF16) || c->num_layers > 4096 ||
+      c->dtype < RA_F32 || c->dtype > RA_E4M3 || c->num_layers > 4096 ||
       (c->layout != RA_LAYOUT_CHRONOLOGICAL && c->layout != RA_LAYOUT_HOLE_FILL &&
        c->layout != RA_LAYOUT_PAGED) ||
       c->policy < RA_POLICY_RANDOM || c->policy > RA_POLICY_EXTERNAL ||
@@ -625,6 +536,8 @@ ra_status ra_config_check(const ra_config* c) {
     if (pages_per_seq(*c) > ra::kMaxPagesLds) return RA_ERR_UNSUPPORTED;
   }
   if (c->head_dim != ra::kHeadDim) return RA_ERR_UNSUPPORTED;
+  // (a hole-fill event moves single rows, whose scales would move with them)
+  if (c->dtype == RA_E4M3 && c->layout == RA_LAYOUT_HOLE_FILL) return RA_ERR_UNSUPPORTED;
   if (c->num_q_heads / c->num_kv_heads > ra::kMaxGroup) return RA_ERR_UNSUPPORTED;
   if (c->evict_every > ra::kMaxEvery) return RA_ERR_UNSUPPORTED;
   // the selection holds every examined slot's score in registers (hole-fill
@@ -668,6 +581,14 @@ int64_t ra_required_slots(const ra_config* c, const int32_t* prompt_lens, int32_
   return total;
 }
 
+size_t ra_pool_bytes(const ra_config* c, int64_t pool_rows) {
+  if (ra_config_check(c) != RA_OK || pool_rows < 0 || pool_rows > (int64_t(1) << 40)) return 0;
+  const size_t row = c->dtype == RA_F32    ? ra::kHeadDim * sizeof(float)
+                     : c->dtype == RA_BF16 ? ra::kHeadDim * 2
+                                           : ra::kHeadDim + 1;   // the codes and a scale
+  return static_cast<size_t>(pool_rows) * row;
+}
+
 size_t ra_meta_bytes(const ra_config* c) {
   if (ra_config_check(c) != RA_OK) return 0;
   return meta_records_bytes(*c) + tables_bytes(*c) + drops_bytes(*c) + arrivals_bytes(*c);
@@ -704,7 +625,7 @@ ra_status ra_cache_create(const ra_config* cfg, void* k_pool, void* v_pool,
   if (!c) return RA_ERR_CAPACITY;
   c->cfg = *cfg;
   c->G = cfg->num_q_heads / cfg->num_kv_heads;
-  c->elem = cfg->dtype == RA_BF16 ? 2 : 4;
+  c->elem = cfg->dtype == RA_BF16 ? 2 : cfg->dtype == RA_E4M3 ? 1 : 4;
   c->kpool = k_pool;
   c->vpool = v_pool;
   c->pos = pos_pool;
@@ -829,6 +750,7 @@ ra_status ra_seq_begin(ra_cache* c, int32_t seq, int32_t prompt_len, uint64_t se
       return hip_fail(e);
     }
     c->mirror[seq] = M;
+    c->rows_change(seq, 0);
     c->update_range();
     return RA_OK;
   }
@@ -857,6 +779,7 @@ ra_status ra_seq_begin(ra_cache* c, int32_t seq, int32_t prompt_len, uint64_t se
   c->free_rows.erase(it);
   if (rest > 0) c->free_rows[base + need] = rest;
   c->mirror[seq] = M;
+  c->rows_change(seq, 0);
   c->update_range();
   return RA_OK;
 }
@@ -965,6 +888,7 @@ ra_status ra_end_step(ra_cache* c, void* stream, int32_t* n_evicted) {
     M.len += 1;
     mirror_plan(M, c->cfg.recent_r, at_trigger(c->cfg, M.step));   // clears a pending move
     due += M.due;
+    if (M.due) c->rows_change(i, M.prompt_len);
     // the pages past the new length are free once the event (launched below,
     // ahead of any later use of them on this stream) has moved their rows
     if (M.due && c->is_paged()) c->shrink(i, M.len);
@@ -979,7 +903,8 @@ ra_status ra_end_step(ra_cache* c, void* stream, int32_t* n_evicted) {
     // that steps of heads with nothing to move run the streaming kernel.
     int n_active = 0;
     for (int i = c->slot_lo; i < c->slot_hi; ++i) n_active += c->mirror[i].active;
-    const bool defer = c->drops && due == n_active && attention_plan(c).whole;
+    // (with block bounds attached a step may read part of the rows only: it moves none)
+    const bool defer = c->drops && !c->bounds && due == n_active && attention_plan(c).whole;
     const int candidates = c->max_candidates_due();
     ra::DueList list;
     if (due <= ra::kDueList) {
@@ -1035,6 +960,7 @@ ra_status ra_graph_mode(ra_cache* c, int32_t on, void* stream) {
     if (!dev[i].active || dev[i].base != c->mirror[i].base || dev[i].cap != c->mirror[i].cap)
       return RA_ERR_STATE;
     c->mirror[i] = dev[i];
+    c->rows_change(i, dev[i].prompt_len);   // events of graph mode
   }
   c->graph = false;
   return RA_OK;
@@ -1061,6 +987,7 @@ ra_status ra_evict_now(ra_cache* c, int32_t seq, void* stream) {
   for (int i = c->slot_lo; i < c->slot_hi; ++i) c->mirror[i].due = 0;
   mirror_plan(M, c->cfg.recent_r, true);
   if (M.due) {
+    c->rows_change(seq, M.prompt_len);
     if (c->is_paged()) c->shrink(seq, M.len);
     ra::DueList list;
     list.slot[list.n++] = seq;
@@ -1118,6 +1045,8 @@ ra_status fast_forward_range(ra_cache* c, int lo, int hi, int32_t n_steps, hipSt
     const ra_status fl = flush_pending(c, s);
     if (fl != RA_OK) return fl;
   }
+  for (int i = lo; i < hi; ++i)
+    if (c->mirror[i].active) c->rows_change(i, c->mirror[i].prompt_len);
   // Runs of steps up to the next trigger of any sequence.  The first pass
   // replays them on a copy of the mirror only, so that a capacity error (rows
   // piling up under the external policy) is reported before any launch; the
@@ -1243,6 +1172,7 @@ ra_status ra_write_rows(ra_cache* c, int32_t seq, const void* dev_k, const void*
   if ((!dev_k || !dev_v) && M.len > 0) return RA_ERR_INVALID_ARG;   // NULL only if empty
   const ra_status fl = flush_pending(c, static_cast<hipStream_t>(stream));
   if (fl != RA_OK) return fl;
+  c->rows_change(seq, 0);
   // positions are left as they are: pass the region's own positions through
   RA_LAUNCH(ra::launch_write_rows(c->shape(), M, seq, M.len, dev_k, dev_v, nullptr,
                                   c->kpool, c->vpool, nullptr, static_cast<hipStream_t>(stream)));
@@ -1369,7 +1299,10 @@ ra_status ra_scored_evict(ra_cache* c, int32_t seq_lo, int32_t seq_hi,
   RA_LAUNCH(ra::launch_plan_range(c->meta, seq_lo, seq_hi, r, s));
   for (int i = c->slot_lo; i < c->slot_hi; ++i) c->mirror[i].due = 0;
   for (int i = seq_lo; i < seq_hi; ++i)
-    if (c->mirror[i].active) mirror_plan(c->mirror[i], r, true);
+    if (c->mirror[i].active) {
+      mirror_plan(c->mirror[i], r, true);
+      if (c->mirror[i].due) c->rows_change(i, 0);   // (the prompt's rows compete too)
+    }
   RA_LAUNCH(by_slot_chunks(c->cfg, seq_lo, seq_hi, [&](int lo, int hi) {
     return ra::launch_compact_drops(c->shape(), c->meta, c->kpool, c->vpool, c->pos, drops,
                                     every, lo, hi, s);

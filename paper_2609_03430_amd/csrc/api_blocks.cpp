@@ -1,0 +1,149 @@
+// C ABI: rows of every head read at once, and block-sparse decode attention.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "cache.h"
+#include "ra_internal.h"
+#include "randattn.h"
+
+using ra::SeqMeta;
+using ra::host::Plan;
+
+namespace {
+
+bool sparse_supported(const ra_config& c) {
+  return c.dtype != RA_F32 && c.layout != RA_LAYOUT_HOLE_FILL;
+}
+
+size_t list_bytes(const ra_config& c, int32_t n_blocks) {
+  const size_t per_head = static_cast<size_t>(std::min(n_blocks, ra::kMaxBlocks));
+  const size_t n = static_cast<size_t>(c.max_seqs) * c.num_kv_heads * per_head * sizeof(int32_t);
+  return (n + 255) / 256 * 256;
+}
+
+}  // namespace
+
+extern "C" {
+
+ra_status ra_export_rows(ra_cache* c, int32_t seq, void* dev_k, void* dev_v, int64_t out_elems,
+                         void* stream) {
+  if (!c || seq < 0 || seq >= c->cfg.max_seqs) return RA_ERR_INVALID_ARG;
+  if (c->graph) return RA_ERR_STATE;   // needs the host mirror (ra_graph_mode)
+  if (c->step_open()) return RA_ERR_STATE;
+  const SeqMeta& M = c->mirror[seq];
+  if (!M.active) return RA_ERR_STATE;
+  if (out_elems < static_cast<int64_t>(M.len) * c->cfg.num_layers * c->cfg.num_kv_heads *
+                      ra::kHeadDim)
+    return RA_ERR_CAPACITY;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const ra_status fl = ra::host::flush_pending(c, s);
+  if (fl != RA_OK) return fl;
+  RA_LAUNCH(ra::launch_export_rows(c->shape(), M, seq, M.len, c->kpool, c->vpool, dev_k, dev_v, s));
+  return RA_OK;
+}
+
+size_t ra_sparse_bytes(const ra_config* c, int64_t pool_rows) {
+  if (ra_config_check(c) != RA_OK || !sparse_supported(*c) || pool_rows <= 0 ||
+      pool_rows % ra::kBlockRows != 0 || pool_rows > (int64_t(1) << 40))
+    return 0;
+  return static_cast<size_t>(
+      ra::host::round_up(pool_rows / ra::kBlockRows * (ra::kBoundsBytes + 1), 256));
+}
+
+size_t ra_sparse_workspace_bytes(const ra_config* c, int32_t n_blocks) {
+  if (ra_config_check(c) != RA_OK || !sparse_supported(*c) || n_blocks < 0) return 0;
+  return ra_workspace_bytes(c) + list_bytes(*c, n_blocks);
+}
+
+ra_status ra_sparse_attach(ra_cache* c, void* bounds, size_t bounds_bytes, void* stream) {
+  if (!c) return RA_ERR_INVALID_ARG;
+  if (!sparse_supported(c->cfg)) return RA_ERR_UNSUPPORTED;
+  if (bounds && (bounds_bytes < ra_sparse_bytes(&c->cfg, c->pool_rows) ||
+                 (reinterpret_cast<uintptr_t>(bounds) & 15u) != 0))
+    return RA_ERR_INVALID_ARG;
+  if (c->graph || c->step_open()) return RA_ERR_STATE;
+  const ra_status fl = ra::host::flush_pending(c, static_cast<hipStream_t>(stream));
+  if (fl != RA_OK) return fl;
+  c->bounds = static_cast<int8_t*>(bounds);
+  c->bounds_built.assign(
+      bounds ? static_cast<size_t>(c->cfg.num_layers) * c->cfg.max_seqs : 0, 0);
+  return RA_OK;
+}
+
+ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int32_t recent_rows,
+                              const void* q, const void* k_new, const void* v_new, void* out,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  if (n_blocks < 0 || recent_rows < 0) return RA_ERR_INVALID_ARG;
+  const ra_status st = ra::host::check_decode(c, layer, q, k_new, v_new, out);
+  if (st != RA_OK) return st;
+  if (!sparse_supported(c->cfg)) return RA_ERR_UNSUPPORTED;
+  if (!c->bounds || c->graph) return RA_ERR_STATE;   // (graph mode: bounds follow the mirror)
+  if (!workspace || workspace_bytes < ra_sparse_workspace_bytes(&c->cfg, n_blocks) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
+    return RA_ERR_INVALID_ARG;
+  // the attended rows of the longest step, and the blocks that need bounds first
+  std::vector<ra::BoundsRange> ranges;
+  int most = 0, n_active = 0, candidates = 0;
+  for (int s = c->slot_lo; s < c->slot_hi; ++s) {
+    const SeqMeta& M = c->mirror[s];
+    if (!M.active) continue;
+    ++n_active;
+    most = std::max(most, ra::attended_blocks(M.len, recent_rows, n_blocks));
+    const int cand = ra::candidate_blocks(M.len, recent_rows);
+    if (cand <= n_blocks) continue;
+    candidates = std::max(candidates, cand);
+    const int built = c->bounds_built[static_cast<size_t>(layer) * c->cfg.max_seqs + s];
+    if (built < cand) ranges.push_back(ra::BoundsRange{s, built, cand});
+  }
+  if (candidates > ra::kMaxBlocks) return RA_ERR_UNSUPPORTED;
+  const hipStream_t hs = static_cast<hipStream_t>(stream);
+  const ra_status grown = ra::host::grow_for_step(c, hs);
+  if (grown != RA_OK) return grown;
+  const ra::Shape sh = c->shape();
+  if (!ranges.empty()) {
+    RA_LAUNCH(ra::launch_block_bounds(sh, c->meta, c->kpool, c->bounds, c->pool_rows, layer,
+                                      ranges.data(), static_cast<int>(ranges.size()), hs));
+    for (const ra::BoundsRange& r : ranges)
+      c->bounds_built[static_cast<size_t>(layer) * c->cfg.max_seqs + r.slot] = r.to;
+  }
+  int32_t* list = static_cast<int32_t*>(workspace);
+  const ra::BlockChoice choice{list, std::min(n_blocks, ra::kMaxBlocks), n_blocks, recent_rows};
+  if (candidates > 0 && n_blocks > 0)
+    RA_LAUNCH(ra::launch_choose_blocks(sh, c->meta, q, c->bounds, c->pool_rows, layer, c->slot_hi,
+                                       choice, list, candidates, hs));
+  c->appended[layer] = 1;
+  ++c->n_appended;
+  if (n_active == 0) return RA_OK;
+  const Plan plan = ra::host::plan_blocks(c, int64_t(most) * ra::kBlockRows,
+                                          n_active * c->cfg.num_kv_heads);
+  const size_t items = static_cast<size_t>(c->cfg.max_seqs) * c->cfg.num_kv_heads * ra::kMaxSplits;
+  ra::AttnLaunch a{};
+  a.meta = c->meta;
+  a.kpool = c->kpool;
+  a.vpool = c->vpool;
+  a.pos = c->pos;
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.out = out;
+  a.ws_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + list_bytes(c->cfg, n_blocks));
+  a.ws_ml = a.ws_o + items * c->G * ra::kHeadDim;
+  a.split_stride = ra::kMaxSplits;
+  a.layer = layer;
+  a.max_seqs = c->slot_hi;
+  a.split_keys = plan.launch_keys();
+  a.max_splits = plan.launch_splits();
+  a.waves = plan.launch_waves();
+  a.arrivals = c->arrivals;
+  const hipError_t e = ra::launch_block_attention(sh, a, choice, hs);
+  if (e != hipSuccess) {
+    c->appended[layer] = 0;
+    --c->n_appended;
+    return ra::host::hip_fail(e);
+  }
+  return RA_OK;
+}
+
+}  // extern "C"

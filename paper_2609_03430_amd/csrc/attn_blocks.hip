@@ -1,0 +1,440 @@
+// Decode attention over blocks of 32 cached rows: every block of an e4m3 cache, or
+// in a block-sparse step the blocks chosen for each KV head and the recent ones, of
+// a bf16 or an e4m3 cache.  The mathematics is that of attention.hip: one pass with
+// an online softmax, S^T = K Q^T and O^T += V^T P^T on the matrix cores, the weights
+// in two bf16 parts, the step's new pair attended and appended.
+//
+// The blocks that a (sequence, KV head) attends to are numbered 0 .. n - 1
+// (attended_blocks); a workgroup takes a run of them, its W wavefronts a W-th of the
+// run each.  The last block holds the step's new row: it is read like any other (it
+// lies inside the head's region or page), and the wavefront that owns it puts the
+// new pair in its place and zeros above it.
+#include "attn_parts.h"
+#include "e4m3.h"
+
+namespace ra {
+namespace {
+
+struct BlockWork : Work {
+  int b0, b1;        // the workgroup's attended blocks
+  int n;             // attended blocks of the head
+  int chosen;        // the first `chosen` come from the list ..
+  int shift;         // .. and block i after them is cached block i + shift
+};
+
+template <bool LIST>
+__device__ __forceinline__ BlockWork locate_blocks(const AttnLaunch& a, const BlockChoice& ch,
+                                                   int Hkv, const Paging& pg) {
+  BlockWork w;
+  w.split = blockIdx.x;
+  w.g = blockIdx.y;
+  w.slot = blockIdx.z;
+  const SeqMeta& M = a.meta[w.slot];
+  w.valid = false;
+  if (!M.active) return w;
+  w.len = M.len;
+  w.n_keys = w.len + 1;
+  w.chosen = w.shift = 0;
+  if constexpr (LIST) {
+    const int cand = candidate_blocks(w.len, ch.recent);
+    if (cand > ch.n_blocks) {
+      w.chosen = ch.n_blocks;
+      w.shift = cand - ch.n_blocks;
+    }
+  }
+  w.n = w.len / kBlockRows + 1 - w.shift;
+  const int per = a.split_keys / kBlockRows;
+  w.b0 = w.split * per;
+  if (w.b0 >= w.n) return w;
+  w.b1 = min(w.b0 + per, w.n);
+  w.nsplit = (w.n + per - 1) / per;
+  w.rm = row_map(M, w.slot, a.layer * Hkv + w.g, pg);
+  w.valid = true;
+  return w;
+}
+
+// Splits of a head, for the merge.
+struct BlockSplits {
+  int recent, n_blocks;
+  __device__ __forceinline__ int operator()(const AttnLaunch& a, int slot) const {
+    const int per = a.split_keys / kBlockRows;
+    return (attended_blocks(a.meta[slot].len, recent, n_blocks) + per - 1) / per;
+  }
+};
+
+// Pools and scales of a launch.
+struct Pools {
+  const void* k;
+  const void* v;
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
+};
+
+// ---- bf16 rows -----------------------------------------------------------------
+
+struct Bf16Rows {
+  using Block = BlockRegs;
+  using Channels = RowChannels;
+  using Query = bf16x8[4];
+
+  static __device__ __forceinline__ void load(Block& b, const Pools& p, int64_t row,
+                                              const LaneMap& lm) {
+    load_block(b, static_cast<const uint16_t*>(p.k) + row * kHeadDim,
+               static_cast<const uint16_t*>(p.v) + row * kHeadDim, 0, lm);
+  }
+  static __device__ __forceinline__ int query_channel(int step, int grp) {
+    return 32 * step + 8 * grp;
+  }
+  // The step's pair, as bf16 in LDS (called by one whole wavefront).
+  struct New {
+    uint16_t k[kHeadDim], v[kHeadDim];
+    __device__ __forceinline__ void stage(const uint16_t* kn, const uint16_t* vn) {
+      const int lane = threadIdx.x & 63;
+      reinterpret_cast<uint32_t*>(k)[lane] = reinterpret_cast<const uint32_t*>(kn)[lane];
+      reinterpret_cast<uint32_t*>(v)[lane] = reinterpret_cast<const uint32_t*>(vn)[lane];
+    }
+    // .. at row `at` of the block, zeros above it
+    __device__ __forceinline__ void patch(Block& b, int at, const LaneMap& lm) const {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (lm.krow[t] == at) {
+#pragma unroll
+          for (int s = 0; s < 4; ++s) b.k[t][s] = ld16(k + lm.kcol + 32 * s);
+        }
+      const int r = at - lm.vrow;
+      if (r < 8) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          uint16_t e8[8];
+          __builtin_memcpy(e8, &b.v[u], 16);
+          const uint16_t x = v[16 * u + lm.vch];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) e8[e] = e < r ? e8[e] : e == r ? x : uint16_t(0);
+          __builtin_memcpy(&b.v[u], e8, 16);
+        }
+      }
+    }
+    __device__ __forceinline__ void append(const AttnLaunch& a, int64_t row,
+                                           uint8_t*, uint8_t*) const {
+      const int lane = threadIdx.x & 63;
+      uint16_t* kp = static_cast<uint16_t*>(a.kpool);
+      uint16_t* vp = static_cast<uint16_t*>(a.vpool);
+      for (int c = lane; c < kHeadDim; c += 64) {
+        kp[row * kHeadDim + c] = k[c];
+        vp[(row & ~int64_t(7)) * kHeadDim + c * 8 + (row & 7)] = v[c];
+      }
+    }
+  };
+  static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const bf16x8 (&q)[4],
+                                                 float scale_log2, int limit) {
+    compute_block(st, b, q, scale_log2, limit);
+  }
+};
+
+// ---- e4m3 rows -------------------------------------------------------------------
+
+// A lane's 16-byte loads hold 16 channels of a key row, two k-steps' operands, and
+// two channels of a value tile, the operands of two output tiles: output tile 2u + h
+// is channels 32u + 2 * (its row) + h.
+struct E4m3Block {
+  u32x4 k[2][2];     // [S tile][64 channels]
+  u32x4 v[4];        // [32 channels]
+  uint64_t vs;       // scale bytes of the lane's eight values' rows
+  uint32_t ks[2];    // scale bytes of its two key rows
+};
+
+struct E4m3Rows {
+  using Block = E4m3Block;
+  struct Channels {
+    static __device__ __forceinline__ int first(int u, int grp) {
+      return 32 * (u >> 1) + 8 * grp + 4 * (u & 1);
+    }
+  };
+
+  static __device__ __forceinline__ void load(Block& b, const Pools& p, int64_t row,
+                                              const LaneMap& lm) {
+    const uint8_t* K = static_cast<const uint8_t*>(p.k) + row * kHeadDim;
+    const uint8_t* V = static_cast<const uint8_t*>(p.v) + row * kHeadDim;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      b.ks[t] = p.k_scale[row + lm.krow[t]];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        b.k[t][s] = ld16(K + lm.krow[t] * kHeadDim + 2 * lm.kcol + 64 * s);
+    }
+    b.vs = *reinterpret_cast<const uint64_t*>(p.v_scale + row + lm.vrow);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      b.v[u] = ld16_stream(V + lm.vrow * kHeadDim + (32 * u + 2 * lm.vch) * 8);
+  }
+  // first channel of a lane's operand at k-step `step`
+  static __device__ __forceinline__ int query_channel(int step, int grp) {
+    return 64 * (step >> 1) + 16 * grp + 8 * (step & 1);
+  }
+
+  struct New {
+    uint8_t k[kHeadDim], v[kHeadDim];
+    uint32_t ks, vs;
+    // quantised as it is written, and attended as it is held
+    __device__ __forceinline__ void stage(const uint16_t* kn, const uint16_t* vn) {
+      const int lane = threadIdx.x & 63;
+      const uint32_t wk = reinterpret_cast<const uint32_t*>(kn)[lane];
+      const uint32_t wv = reinterpret_cast<const uint32_t*>(vn)[lane];
+      uint32_t mk = max(row_magnitude(bf16_low(wk)), row_magnitude(bf16_high(wk)));
+      uint32_t mv = max(row_magnitude(bf16_low(wv)), row_magnitude(bf16_high(wv)));
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        mk = max(mk, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mk), o, 64)));
+        mv = max(mv, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mv), o, 64)));
+      }
+      const uint32_t bk = e4m3_scale_byte(mk), bv = e4m3_scale_byte(mv);
+      const float ik = e4m3_inverse(bk), iv = e4m3_inverse(bv);
+      reinterpret_cast<uint16_t*>(k)[lane] =
+          static_cast<uint16_t>(e4m3_pack2<false>(e4m3_clamp(bf16_low(wk) * ik, bk),
+                                                  e4m3_clamp(bf16_high(wk) * ik, bk), 0u));
+      reinterpret_cast<uint16_t*>(v)[lane] =
+          static_cast<uint16_t>(e4m3_pack2<false>(e4m3_clamp(bf16_low(wv) * iv, bv),
+                                                  e4m3_clamp(bf16_high(wv) * iv, bv), 0u));
+      if (lane == 0) {
+        ks = bk;
+        vs = bv;
+      }
+    }
+    __device__ __forceinline__ void patch(Block& b, int at, const LaneMap& lm) const {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (lm.krow[t] == at) {
+          b.ks[t] = ks;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) b.k[t][s] = ld16(k + 2 * lm.kcol + 64 * s);
+        }
+      const int r = at - lm.vrow;
+      if (r < 8) {
+        const int n = r < 0 ? 0 : r;                     // cached rows of the tile
+        const uint64_t below = (uint64_t(1) << (8 * n)) - 1;
+        b.vs = (b.vs & below) | (r >= 0 ? static_cast<uint64_t>(vs) << (8 * n) : 0);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          uint64_t w[2];
+          __builtin_memcpy(w, &b.v[u], 16);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint64_t x = v[32 * u + 2 * lm.vch + h];
+            w[h] = (w[h] & below) | (r >= 0 ? x << (8 * n) : 0);
+          }
+          __builtin_memcpy(&b.v[u], w, 16);
+        }
+      }
+    }
+    __device__ __forceinline__ void append(const AttnLaunch& a, int64_t row,
+                                           uint8_t* k_scale, uint8_t* v_scale) const {
+      const int lane = threadIdx.x & 63;
+      uint8_t* kp = static_cast<uint8_t*>(a.kpool);
+      uint8_t* vp = static_cast<uint8_t*>(a.vpool);
+      reinterpret_cast<uint16_t*>(kp + row * kHeadDim)[lane] =
+          reinterpret_cast<const uint16_t*>(k)[lane];
+      for (int c = lane; c < kHeadDim; c += 64)
+        vp[(row & ~int64_t(7)) * kHeadDim + c * 8 + (row & 7)] = v[c];
+      if (lane == 0) {
+        k_scale[row] = static_cast<uint8_t>(ks);
+        v_scale[row] = static_cast<uint8_t>(vs);
+      }
+    }
+  };
+
+  // Eight codes of one scale to the bf16 numbers that they stand for (exact).
+  static __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale) {
+    const f32x2 a = e4m3_unpack2<false>(w0), b = e4m3_unpack2<true>(w0);
+    const f32x2 c = e4m3_unpack2<false>(w1), d = e4m3_unpack2<true>(w1);
+    u32x4 r;
+    r.x = bf16_pack_exact(a[0] * scale, a[1] * scale);
+    r.y = bf16_pack_exact(b[0] * scale, b[1] * scale);
+    r.z = bf16_pack_exact(c[0] * scale, c[1] * scale);
+    r.w = bf16_pack_exact(d[0] * scale, d[1] * scale);
+    return as_bf16x8(r);
+  }
+
+  // compute_block over the values that the rows stand for: a key's scale goes with
+  // its codes, a value's with its weight.
+  static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const bf16x8 (&q)[4],
+                                                 float scale_log2, int limit) {
+    f32x4 s[2] = {};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float scale = e4m3_scale(b.ks[t]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(b.k[t][i].x, b.k[t][i].y, scale),
+                                                       q[2 * i], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(b.k[t][i].z, b.k[t][i].w, scale),
+                                                       q[2 * i + 1], s[t], 0, 0, 0);
+      }
+    }
+    const int grp = (threadIdx.x & 63) >> 4;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = s[0][i] * scale_log2;
+      x[4 + i] = s[1][i] * scale_log2;
+    }
+    if (limit < 32) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (8 * grp + e >= limit) x[e] = kNegInf;
+    }
+    float bm = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
+    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
+    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
+    const float mn = fmaxf(st.m, bm);
+    const float alpha = exp2f(st.m - mn);
+    bf16x8 p_hi, p_lo;
+    float psum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float pf = exp2f(x[e] - mn);
+      const float pv = pf * e4m3_scale(static_cast<uint32_t>(b.vs >> (8 * e)) & 255u);
+      const __bf16 hi = static_cast<__bf16>(pv);
+      p_hi[e] = hi;
+      p_lo[e] = static_cast<__bf16>(pv - static_cast<float>(hi));
+      psum += pf;
+    }
+    st.l = st.l * alpha + psum;
+    st.m = mn;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const u32x4 w = b.v[u >> 1];
+      const bf16x8 v = u & 1 ? to_bf16(w.z, w.w, 1.f) : to_bf16(w.x, w.y, 1.f);
+      st.acc[u] *= alpha;
+      st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_hi, st.acc[u], 0, 0, 0);
+      st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_lo, st.acc[u], 0, 0, 0);
+    }
+  }
+
+  // tiles 2u and 2u + 1 hold alternate channels: to runs of four
+  static __device__ __forceinline__ void gather_channels(Softmax& st) {
+#pragma unroll
+    for (int u = 0; u < 8; u += 2) {
+      const f32x4 a = st.acc[u], b = st.acc[u + 1];
+      st.acc[u] = f32x4{a[0], b[0], a[1], b[1]};
+      st.acc[u + 1] = f32x4{a[2], b[2], a[3], b[3]};
+    }
+  }
+};
+
+template <typename R, int W, int MINW, bool PAGED, bool LIST>
+__global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
+    AttnLaunch a, BlockChoice ch, Paging pg, uint8_t* k_scale, uint8_t* v_scale, int G, int Hq,
+    int Hkv, float scale_log2) {
+  __shared__ float s_m[W][kMaxGroup];
+  __shared__ float s_l[W][kMaxGroup];
+  __shared__ float s_o[W][kMaxGroup][kHeadDim];
+  __shared__ __align__(16) typename R::New s_new;
+  const BlockWork w = locate_blocks<LIST>(a, ch, Hkv, pg);
+  if (!w.valid) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, qi = lane & 15, grp = lane >> 4;
+  const LaneMap lm = lane_map();
+  const Pools pools{a.kpool, a.vpool, k_scale, v_scale};
+  const int per = (w.b1 - w.b0 + W - 1) / W;
+  const int b0 = __builtin_amdgcn_readfirstlane(w.b0 + wave * per);
+  const int b1 = __builtin_amdgcn_readfirstlane(min(b0 + per, w.b1));
+  const bool has = b0 < b1;
+  const bool owns_last = has && b1 == w.n;
+  const int32_t* list = nullptr;
+  if constexpr (LIST) list = ch.list + (static_cast<int64_t>(w.slot) * Hkv + w.g) * ch.stride;
+  const auto load = [&](typename R::Block& b, int i) {
+    int cached = i + w.shift;
+    if constexpr (LIST) {
+      if (i < w.chosen) cached = list[i];
+    }
+    R::load(b, pools, pool_row<PAGED>(w.rm, cached * kBlockRows), lm);
+  };
+
+  Softmax st;
+  st.m = kNoScore;
+  st.l = 0.f;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) st.acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (has) {
+    bf16x8 qop[4];
+    const uint16_t* qrow = static_cast<const uint16_t*>(a.q) +
+                           (static_cast<int64_t>(w.slot) * Hq + w.g * G + (qi < G ? qi : 0)) * kHeadDim;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const u32x4 z = {0u, 0u, 0u, 0u};
+      const u32x4 x = ld16(qrow + R::query_channel(s, grp));
+      qop[s] = as_bf16x8(qi < G ? x : z);
+    }
+    if (owns_last) {
+      const int64_t src = (static_cast<int64_t>(w.slot) * Hkv + w.g) * kHeadDim;
+      s_new.stage(static_cast<const uint16_t*>(a.k_new) + src,
+                  static_cast<const uint16_t*>(a.v_new) + src);
+    }
+    const int last = b1 - 1;
+    typename R::Block x0, x1;
+    load(x0, b0);
+    load(x1, min(b0 + 1, last));
+    int i = b0;
+    for (; i + 1 < last; i += 2) {
+      R::compute(st, x0, qop, scale_log2, 32);
+      load(x0, min(i + 2, last));
+      R::compute(st, x1, qop, scale_log2, 32);
+      load(x1, min(i + 3, last));
+    }
+    if (i < last) {
+      R::compute(st, x0, qop, scale_log2, 32);
+      x0 = x1;
+    }
+    int limit = 32;
+    if (owns_last) {
+      const int at = w.len % kBlockRows;
+      s_new.patch(x0, at, lm);
+      limit = at + 1;
+    }
+    R::compute(st, x0, qop, scale_log2, limit);
+    st.l += __shfl_xor(st.l, 16, 64);
+    st.l += __shfl_xor(st.l, 32, 64);
+  }
+  if constexpr (!std::is_same_v<R, Bf16Rows>) R::gather_channels(st);
+  finish_item<uint16_t, W, true, BlockSplits, typename R::Channels>(
+      a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o,
+      LIST ? BlockSplits{ch.recent, ch.n_blocks} : BlockSplits{0, 1 << 30});
+  if (owns_last) {
+    const int64_t row = pool_row<PAGED>(w.rm, w.len);
+    s_new.append(a, row, k_scale, v_scale);
+    if (lane == 0) a.pos[row] = a.meta[w.slot].prompt_len + a.meta[w.slot].step;
+  }
+}
+
+template <typename R, bool PAGED, bool LIST>
+void launch_blocks(const Shape& sh, const AttnLaunch& a, const BlockChoice& ch, hipStream_t s) {
+  const dim3 grid(a.max_splits, sh.Hkv, a.max_seqs);
+  const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(kHeadDim));
+  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, 1, PAGED, LIST>), grid, dim3(256), 0, s, a, ch,
+                     sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
+}
+
+}  // namespace
+
+hipError_t launch_attention_e4m3(const Shape& sh, const AttnLaunch& a, hipStream_t s) {
+  const BlockChoice none{nullptr, 0, 0, 0};
+  if (sh.pg.tables) launch_blocks<E4m3Rows, true, false>(sh, a, none, s);
+  else launch_blocks<E4m3Rows, false, false>(sh, a, none, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_block_attention(const Shape& sh, const AttnLaunch& a, const BlockChoice& ch,
+                                  hipStream_t s) {
+  if (sh.dtype == 2) {
+    if (sh.pg.tables) launch_blocks<E4m3Rows, true, true>(sh, a, ch, s);
+    else launch_blocks<E4m3Rows, false, true>(sh, a, ch, s);
+  } else {
+    if (sh.pg.tables) launch_blocks<Bf16Rows, true, true>(sh, a, ch, s);
+    else launch_blocks<Bf16Rows, false, true>(sh, a, ch, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ra

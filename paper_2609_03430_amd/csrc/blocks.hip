@@ -1,0 +1,309 @@
+// Choice of the blocks of a block-sparse decode step: bounds of each block's keys,
+// kept in 8 bits, and for each KV head the blocks whose bounds score highest
+// against the step's queries.
+//
+// A block is 32 cached rows.  With hi_c and lo_c the largest and smallest value of
+// channel c over its keys (a NaN counts as 0, an infinity as the largest bf16
+// number) and 2^t the power of two that brings max_c max(|hi_c|, |lo_c|) into
+// (63.5, 127] (t in [-60, 50]), the bounds are held as H_c = ceil(hi_c / 2^t) and
+// L_c = floor(lo_c / 2^t), rounded outwards so that they still bound the keys.
+// A query row is brought to Q_c = rint(q_c / 2^u) likewise, and
+//   score = max over the group's queries of 2^(t+u) * sum_c max(Q_c H_c, Q_c L_c),
+// an upper bound of its products with the block's keys but for Q's rounding.  The
+// sums are of integers and exact, and so is the power of two in fp32: the choice does
+// not depend on the order of anything.
+#include "attn_parts.h"
+#include "e4m3.h"
+#include "select.h"
+
+namespace ra {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kMaxBf16 = 3.3895313892515355e38f;
+
+__device__ __forceinline__ float finite_bf16(float x) {
+  x = x == x ? x : 0.f;
+  return fminf(fmaxf(x, -kMaxBf16), kMaxBf16);
+}
+
+// t of a largest magnitude: its fp32 exponent less 6 where its fraction is at most
+// 127/64, else less 5 (the sum carries), within [-60, 50].
+__device__ __forceinline__ int unit_exponent(uint32_t amax_bits) {
+  const int t = static_cast<int>((amax_bits + 0x01ffffu) >> 23) - 127 - 6;
+  return min(max(t, -60), 50);
+}
+
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((e + 127) << 23); }
+
+__device__ __forceinline__ uint32_t pack_int8(float a, float b, float c, float d) {
+  const auto byte = [](float x) {
+    return static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(x, -127.f), 127.f))) & 255u;
+  };
+  return byte(a) | byte(b) << 8 | byte(c) << 16 | byte(d) << 24;
+}
+
+struct BoundsBatch {
+  BoundsRange r[kBoundsBatch];
+};
+
+// One wavefront per block: lane (c8, rows) reads eight channels of eight rows, the
+// four row groups join by shuffles.  Bound by HBM: the key rows, once per row that an
+// event or a write has changed.  Grid: (ceil(blocks / 4), Hkv, ranges).
+template <bool E4M3, bool PAGED>
+__global__ __launch_bounds__(256) void block_bounds_kernel(
+    const SeqMeta* __restrict__ meta, const void* __restrict__ kpool,
+    const uint8_t* __restrict__ k_scale, int8_t* __restrict__ bounds, int8_t* __restrict__ units,
+    int layer, int Hkv, Paging pg, BoundsBatch batch) {
+  const BoundsRange range = batch.r[blockIdx.z];
+  const int b = range.from + static_cast<int>(blockIdx.x) * 4 +
+                __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (b >= range.to) return;
+  const SeqMeta& M = meta[range.slot];
+  const RowMap rm = row_map(M, range.slot, layer * Hkv + static_cast<int>(blockIdx.y), pg);
+  const int64_t row0 = pool_row<PAGED>(rm, b * kBlockRows);
+  const int lane = threadIdx.x & 63, c8 = lane & 15, r4 = lane >> 4;
+  float hi[8], lo[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    hi[c] = -kMaxBf16;
+    lo[c] = kMaxBf16;
+  }
+  const auto take = [&](int c, float x) {
+    x = finite_bf16(x);
+    hi[c] = fmaxf(hi[c], x);
+    lo[c] = fminf(lo[c], x);
+  };
+  if constexpr (E4M3) {
+    uint2 w[8];
+    uint32_t s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t row = row0 + r4 + 4 * e;
+      w[e] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(kpool) +
+                                             row * kHeadDim + 8 * c8);
+      s[e] = k_scale[row];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float scale = e4m3_scale(s[e]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t x = i ? w[e].y : w[e].x;
+        const f32x2 p = e4m3_unpack2<false>(x), q = e4m3_unpack2<true>(x);
+        take(4 * i, p[0] * scale);
+        take(4 * i + 1, p[1] * scale);
+        take(4 * i + 2, q[0] * scale);
+        take(4 * i + 3, q[1] * scale);
+      }
+    }
+  } else {
+    u32x4 w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      w[e] = ld16(static_cast<const uint16_t*>(kpool) + (row0 + r4 + 4 * e) * kHeadDim + 8 * c8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        take(2 * i, bf16_low(w[e][i]));
+        take(2 * i + 1, bf16_high(w[e][i]));
+      }
+  }
+  uint32_t amax = 0;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+      hi[c] = fmaxf(hi[c], __shfl_xor(hi[c], o, 64));
+      lo[c] = fminf(lo[c], __shfl_xor(lo[c], o, 64));
+    }
+    amax = max(amax, max(__float_as_uint(fabsf(hi[c])), __float_as_uint(fabsf(lo[c]))));
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1)
+    amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
+  const int t = unit_exponent(amax);
+  const float inv = pow2(-t);
+  if (r4 < 2) {
+    float v[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = r4 == 0 ? ceilf(hi[c] * inv) : floorf(lo[c] * inv);
+    uint2 w;
+    w.x = pack_int8(v[0], v[1], v[2], v[3]);
+    w.y = pack_int8(v[4], v[5], v[6], v[7]);
+    *reinterpret_cast<uint2*>(bounds + row0 / kBlockRows * kBoundsBytes + kHeadDim * r4 + 8 * c8) =
+        w;
+  }
+  if (lane == 0) units[row0 / kBlockRows] = static_cast<int8_t>(t);
+}
+
+// One workgroup per (sequence, KV head): the wavefronts score sixteen blocks at a time
+// (v_mfma_i32_16x16x64_i8: blocks x [H | L] against [max(Q, 0); min(Q, 0)] for the
+// group's queries), the scores go to LDS, and a radix select (select.h) finds the
+// n_blocks highest, the lowest index first among equals.
+// Bound by the bounds' bytes where they are many and by the selection's passes where
+// they are few.
+template <int NT, int KPT, bool PAGED>
+__global__ __launch_bounds__(NT) void choose_blocks_kernel(
+    const SeqMeta* __restrict__ meta, const uint16_t* __restrict__ q,
+    const int8_t* __restrict__ bounds, const int8_t* __restrict__ units, int layer, int Hq,
+    int Hkv, int G, Paging pg, BlockChoice ch, int32_t* __restrict__ list) {
+  extern __shared__ uint32_t keys[];           // one per candidate, ascending from the best
+  __shared__ SelectShared sel_sh;
+  const int g = blockIdx.x, slot = blockIdx.y;
+  const SeqMeta& M = meta[slot];
+  if (!M.active) return;
+  const int cand = candidate_blocks(M.len, ch.recent);
+  if (cand <= ch.n_blocks) return;
+  const int t = threadIdx.x, lane = t & 63, r = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const RowMap rm = row_map(M, slot, layer * Hkv + g, pg);
+
+  // the group's queries: lane (r, grp) holds channels 64 s + 16 grp .. + 15 of query r
+  i32x4 pos[2], neg[2];
+  int u;
+  {
+    const uint16_t* row = q + (static_cast<int64_t>(slot) * Hq + g * G + (r < G ? r : 0)) * kHeadDim;
+    float x[2][16];
+    uint32_t amax = 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 w = ld16(row + 64 * s + 16 * grp + 8 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[s][8 * h + 2 * i] = finite_bf16(bf16_low(w[i]));
+          x[s][8 * h + 2 * i + 1] = finite_bf16(bf16_high(w[i]));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          amax = max(amax, __float_as_uint(fabsf(x[s][8 * h + i])));
+      }
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1)
+      amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
+    u = unit_exponent(amax);
+    const float inv = pow2(-u);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = rintf(x[s][4 * i + j] * inv);
+        pos[s][i] = static_cast<int>(pack_int8(fmaxf(y[0], 0.f), fmaxf(y[1], 0.f),
+                                               fmaxf(y[2], 0.f), fmaxf(y[3], 0.f)));
+        neg[s][i] = static_cast<int>(pack_int8(fminf(y[0], 0.f), fminf(y[1], 0.f),
+                                               fminf(y[2], 0.f), fminf(y[3], 0.f)));
+      }
+  }
+
+  for (int b0 = 16 * wave; b0 < cand; b0 += NT / 4) {
+    const int64_t at = pool_row<PAGED>(rm, min(b0 + r, cand - 1) * kBlockRows) / kBlockRows;
+    const int8_t* src = bounds + at * kBoundsBytes + 16 * grp;
+    i32x4 h[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) h[s] = *reinterpret_cast<const i32x4*>(src + 64 * s);
+    const int unit = units[at];
+    i32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(h[s], s < 2 ? pos[s] : neg[s - 2], sum, 0, 0, 0);
+    // lane (query r, grp): blocks b0 + 4 grp + i
+    float best[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = u + __shfl(unit, 4 * grp + i, 64);
+      best[i] = r < G ? ldexpf(static_cast<float>(sum[i]), e) : kNegInf;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) best[i] = fmaxf(best[i], __shfl_xor(best[i], o, 64));
+    }
+    if (r < 4) {
+      const int b = b0 + 4 * grp + r;
+      const float x = r == 0 ? best[0] : r == 1 ? best[1] : r == 2 ? best[2] : best[3];
+      const uint32_t bits = __float_as_uint(x);      // descending order of the scores
+      if (b < cand) keys[b] = bits >> 31 ? bits : ~(bits | 0x80000000u);
+    }
+  }
+  __syncthreads();
+
+  uint64_t key[KPT];
+  uint32_t tie[KPT], valid = 0;
+#pragma unroll
+  for (int i = 0; i < KPT; ++i) {
+    const int b = t * KPT + i;
+    tie[i] = static_cast<uint32_t>(b);
+    key[i] = b < cand ? keys[b] : 0u;
+    if (b < cand) valid |= 1u << i;
+  }
+  const uint32_t chosen = select_smallest<NT, KPT, 32>(key, tie, valid, ch.n_blocks, sel_sh);
+  const int mine = __popc(chosen), incl = wave_inclusive_scan(mine);
+  if (lane == 63) sel_sh.wave_tot[wave] = incl;
+  __syncthreads();
+  int k = incl - mine;
+  for (int w = 0; w < wave; ++w) k += sel_sh.wave_tot[w];
+  int32_t* dst = list + (static_cast<int64_t>(slot) * Hkv + g) * ch.stride;
+#pragma unroll
+  for (int i = 0; i < KPT; ++i)
+    if ((chosen >> i) & 1) dst[k++] = t * KPT + i;
+}
+
+template <int NT, int KPT>
+void launch_choose(const Shape& sh, const SeqMeta* meta, const void* q, const int8_t* bounds,
+                   const int8_t* units, int layer, int max_seqs, const BlockChoice& ch,
+                   int32_t* list, int max_candidates, hipStream_t s) {
+  const auto kernel = sh.pg.tables ? choose_blocks_kernel<NT, KPT, true>
+                                   : choose_blocks_kernel<NT, KPT, false>;
+  hipLaunchKernelGGL(kernel, dim3(sh.Hkv, max_seqs), dim3(NT),
+                     sizeof(uint32_t) * static_cast<size_t>(max_candidates), s, meta,
+                     static_cast<const uint16_t*>(q), bounds, units, layer, sh.Hq, sh.Hkv, sh.G,
+                     sh.pg, ch, list);
+}
+
+}  // namespace
+
+hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void* kpool,
+                               int8_t* bounds, int64_t pool_rows, int layer,
+                               const BoundsRange* ranges, int n, hipStream_t s) {
+  int8_t* units = bounds + pool_rows / kBlockRows * kBoundsBytes;
+  const auto kernel =
+      sh.dtype == 2 ? (sh.pg.tables ? block_bounds_kernel<true, true>
+                                    : block_bounds_kernel<true, false>)
+                    : (sh.pg.tables ? block_bounds_kernel<false, true>
+                                    : block_bounds_kernel<false, false>);
+  for (int i0 = 0; i0 < n; i0 += kBoundsBatch) {
+    BoundsBatch b{};
+    const int k = std::min(kBoundsBatch, n - i0);
+    int most = 0;
+    for (int i = 0; i < k; ++i) {
+      b.r[i] = ranges[i0 + i];
+      most = std::max(most, b.r[i].to - b.r[i].from);
+    }
+    hipLaunchKernelGGL(kernel, dim3((most + 3) / 4, sh.Hkv, k), dim3(256), 0, s, meta, kpool,
+                       sh.k_scale, bounds, units, layer, sh.Hkv, sh.pg, b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q,
+                                const int8_t* bounds, int64_t pool_rows, int layer, int max_seqs,
+                                const BlockChoice& ch, int32_t* list, int max_candidates,
+                                hipStream_t s) {
+  const int8_t* units = bounds + pool_rows / kBlockRows * kBoundsBytes;
+#define RA_CHOOSE(NT, KPT)                                                                  \
+  launch_choose<NT, KPT>(sh, meta, q, bounds, units, layer, max_seqs, ch, list, max_candidates, s)
+  if (max_candidates <= 256) RA_CHOOSE(256, 1);
+  else if (max_candidates <= 1024) RA_CHOOSE(1024, 1);
+  else if (max_candidates <= 4096) RA_CHOOSE(1024, 4);
+  else if (max_candidates <= kMaxBlocks) RA_CHOOSE(1024, 16);
+  else return hipErrorInvalidValue;
+#undef RA_CHOOSE
+  return hipGetLastError();
+}
+
+}  // namespace ra

@@ -23,6 +23,7 @@
 //      the positions travel with the rows).
 #include <algorithm>
 
+#include "e4m3.h"
 #include "philox.h"
 #include "ra_internal.h"
 #include "select.h"
@@ -726,6 +727,194 @@ __global__ __launch_bounds__(NT) void move_chunks_kernel(
   }
 }
 
+// ---- e4m3 rows -----------------------------------------------------------------
+
+// Eight consecutive codes of a channel, from code `off` (0..7) of the sixteen
+// that two adjacent value tiles hold.
+__device__ __forceinline__ uint64_t codes_at(uint64_t a, uint64_t b, int off) {
+  return off ? a >> (8 * off) | b << (64 - 8 * off) : a;
+}
+
+// compact_rows for e4m3 rows: keys, values and scale bytes of destination rows
+// [d0, new_len) (positions move with the selection).  Units of 16 bytes: 16
+// channels of a key row, or two channels of a value tile; CHUNK * 8 of each to a
+// round, as many bytes in flight per row as the rows have.
+template <int NT, int CHUNK, typename Rows, typename Loaded = NoHook>
+__device__ __forceinline__ void compact_rows_e4m3(const int* f, int m, int* src_of, int d0,
+                                                  int new_len, int old_len, const Rows& row,
+                                                  uint8_t* __restrict__ kpool,
+                                                  uint8_t* __restrict__ vpool,
+                                                  uint8_t* __restrict__ kscale,
+                                                  uint8_t* __restrict__ vscale,
+                                                  const Loaded& loaded = Loaded()) {
+  static_assert(CHUNK % 8 == 0 && CHUNK <= NT, "a chunk is whole value tiles, one row per thread");
+  constexpr int kUnits = CHUNK * 8;
+  constexpr int kPer = kUnits / NT;
+  static_assert(kPer * NT == kUnits, "every thread has the same units");
+  const int t = threadIdx.x;
+  for (int j0 = d0 & ~7; j0 < new_len; j0 += CHUNK) {
+    if (t < CHUNK) src_of[t] = j0 + t + count_le(f, m, j0 + t);
+    __syncthreads();
+    const bool mine = t < CHUNK && j0 + t >= d0 && j0 + t < new_len;
+    uint8_t ks = 0, vs = 0;
+    if (mine) {
+      const int64_t src = row(src_of[t]);
+      ks = kscale[src];
+      vs = vscale[src];
+    }
+    u32x4 kbuf[kPer];
+    uint64_t vbuf[kPer][2];
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int u = t + q * NT, r = u / 8, j = j0 + r;
+      if (j >= d0 && j < new_len)
+        kbuf[q] = load_stream(kpool + row(src_of[r]) * kHeadDim + u % 8 * 16);
+    }
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int u = t + q * NT, tile = u / 64, ch = u % 64 * 2, jt = tile * 8;
+      if (j0 + jt < new_len) {
+        const int s0 = src_of[jt], s_last = src_of[jt + 7];
+        if (s_last - s0 == 7 && s_last < old_len) {
+          // consecutive sources: one or two adjacent tiles, the same offset for
+          // the whole wavefront
+          u32x4 a = *reinterpret_cast<const u32x4*>(vpool + vt_index(row(s0 & ~7), ch));
+          u32x4 b = a;
+          if (s0 & 7)
+            b = *reinterpret_cast<const u32x4*>(vpool + vt_index(row((s0 & ~7) + 8), ch));
+          uint64_t wa[2], wb[2];
+          __builtin_memcpy(wa, &a, 16);
+          __builtin_memcpy(wb, &b, 16);
+          vbuf[q][0] = codes_at(wa[0], wb[0], s0 & 7);
+          vbuf[q][1] = codes_at(wa[1], wb[1], s0 & 7);
+        } else {
+          uint64_t w0 = 0, w1 = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int sj = src_of[jt + e];
+            if (sj < old_len) {
+              const uint8_t* src = vpool + vt_index(row(sj), ch);
+              w0 |= static_cast<uint64_t>(src[0]) << (8 * e);
+              w1 |= static_cast<uint64_t>(src[8]) << (8 * e);
+            }
+          }
+          vbuf[q][0] = w0;
+          vbuf[q][1] = w1;
+        }
+      }
+    }
+    // every load of this chunk has returned before any thread writes
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    loaded();
+
+    if (mine) {
+      const int64_t dst = row(j0 + t);
+      kscale[dst] = ks;
+      vscale[dst] = vs;
+    }
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int u = t + q * NT, j = j0 + u / 8;
+      if (j >= d0 && j < new_len)
+        store_stream(kpool + row(j) * kHeadDim + u % 8 * 16, kbuf[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      const int u = t + q * NT, tile = u / 64, ch = u % 64 * 2;
+      if (j0 + tile * 8 < new_len) {
+        u32x4 w;
+        __builtin_memcpy(&w, vbuf[q], 16);
+        store_stream(vpool + vt_index(row(j0 + tile * 8), ch), w);
+      }
+    }
+  }
+}
+
+// The moves of an event of an e4m3 cache, after a positions-only selection that
+// left each head's drop list in its rows of positions past the new length: one
+// workgroup per head of the slots given, or with CHUNKED a workgroup per CHUNK
+// rows, handed over as in move_chunks_kernel.  A second launch rather than a
+// build of the selection for these rows: it adds 3 us to an event, and a head's
+// rows are half as many bytes.
+template <int NT, int CHUNK, bool PAGED, bool CHUNKED>
+__global__ __launch_bounds__(NT) void move_e4m3_kernel(
+    const SeqMeta* __restrict__ meta, uint8_t* __restrict__ kpool, uint8_t* __restrict__ vpool,
+    uint8_t* __restrict__ kscale, uint8_t* __restrict__ vscale, const int32_t* __restrict__ pos,
+    int L, int Hkv, int n_chunks, int slot_lo, DueList due, Paging pg,
+    uint32_t* __restrict__ sync_words) {
+  __shared__ int f[kMaxEvery];
+  __shared__ int src_of[CHUNK];
+  __shared__ int tbl[PAGED ? kMaxPagesLds : 1];
+  __shared__ int s_chunk;
+  const int per_seq = L * Hkv;
+  const int head = static_cast<int>(blockIdx.x) / n_chunks;
+  const int slot = due.n ? due.slot[head / per_seq] : slot_lo + head / per_seq;
+  const int lg = head % per_seq;
+  const SeqMeta& M = meta[slot];
+  if (!M.active || !M.due) return;
+  const int old_len = M.plan_len, new_len = M.len, m = old_len - new_len;
+  if (m <= 0 || m > kMaxEvery) return;
+  if (CHUNKED && threadIdx.x == 0)
+    s_chunk = static_cast<int>(__hip_atomic_fetch_add(sync_words + head, 1u, __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT) & 31u);
+  RegionRows rrow{M.base + static_cast<int64_t>(lg) * M.cap};
+  PagedRows prow{};
+  if constexpr (PAGED) {
+    const int32_t* table = pg.tables + static_cast<int64_t>(slot) * pg.pages_per_seq;
+    const int n_pages = (old_len + (1 << pg.page_shift) - 1) >> pg.page_shift;
+    for (int i = threadIdx.x; i < n_pages; i += NT) tbl[i] = table[i];
+    __syncthreads();
+    prow = PagedRows{tbl, pg.group_rows, static_cast<int64_t>(lg) << pg.page_shift,
+                     pg.page_shift};
+  }
+  for (int k = threadIdx.x; k < m; k += NT) {
+    if constexpr (PAGED) f[k] = pos[prow(new_len + k)] - k;
+    else f[k] = pos[rrow(new_len + k)] - k;
+  }
+  __syncthreads();
+  const int chunk = CHUNKED ? __builtin_amdgcn_readfirstlane(s_chunk) : 0;
+  const int d0 = __builtin_amdgcn_readfirstlane(f[0]);
+  const int j0 = (d0 & ~7) + chunk * CHUNK;
+  if (j0 < new_len) {
+    const int first = max(d0, j0), end = CHUNKED ? min(new_len, j0 + CHUNK) : new_len;
+    const auto move = [&](const auto& row) {
+      if constexpr (CHUNKED)
+        compact_rows_e4m3<NT, CHUNK>(f, m, src_of, first, end, old_len, row, kpool, vpool, kscale,
+                                     vscale, ChunkLoaded{sync_words + head, chunk});
+      else
+        compact_rows_e4m3<NT, CHUNK>(f, m, src_of, first, end, old_len, row, kpool, vpool, kscale,
+                                     vscale);
+    };
+    if constexpr (PAGED) move(prow);
+    else move(rrow);
+  }
+  if (CHUNKED && threadIdx.x == 0) {
+    uint32_t* word = sync_words + head;
+    const uint32_t before =
+        __hip_atomic_fetch_add(word, 32u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (((before >> 5) & 31u) == static_cast<uint32_t>(n_chunks - 1))
+      __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+template <bool PAGED>
+void launch_move_e4m3(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                      const int32_t* pos, int slot_lo, int slot_hi, int n_chunks, hipStream_t s) {
+  const DueList due = sh.due ? *sh.due : DueList{};
+  const int heads = (due.n ? due.n : slot_hi - slot_lo) * sh.L * sh.Hkv;
+  uint8_t* k = static_cast<uint8_t*>(kpool);
+  uint8_t* v = static_cast<uint8_t*>(vpool);
+  if (n_chunks > 0)
+    hipLaunchKernelGGL((move_e4m3_kernel<1024, event_chunk_rows(2), PAGED, true>),
+                       dim3(heads * n_chunks), dim3(1024), 0, s, meta, k, v, sh.k_scale,
+                       sh.v_scale, pos, sh.L, sh.Hkv, n_chunks, slot_lo, due, sh.pg, sh.move_sync);
+  else
+    hipLaunchKernelGGL((move_e4m3_kernel<1024, event_chunk_rows(2), PAGED, false>), dim3(heads),
+                       dim3(1024), 0, s, meta, k, v, sh.k_scale, sh.v_scale, pos, sh.L, sh.Hkv, 1,
+                       slot_lo, due, sh.pg, nullptr);
+}
+
 template <int NT, int KPT, bool POS_ONLY, int LAYOUT>
 hipError_t launch_layout(const Shape& sh, const SeqMeta* meta, void* kpool,
                          void* vpool, int32_t* pos, int slot_lo, int slot_hi,
@@ -733,7 +922,7 @@ hipError_t launch_layout(const Shape& sh, const SeqMeta* meta, void* kpool,
                          bool lists_in_pos) {
   const DueList due = sh.due ? *sh.due : DueList{};
   const dim3 grid((due.n ? due.n : slot_hi - slot_lo) * sh.L * sh.Hkv);
-  if (sh.dtype == 1) {
+  if (sh.dtype != 0) {   // (an e4m3 cache's selections are positions-only)
     hipLaunchKernelGGL((evict_kernel<NT, KPT, uint16_t, POS_ONLY, LAYOUT>), grid,
                        dim3(NT), 0, s, meta, static_cast<uint16_t*>(kpool),
                        static_cast<uint16_t*>(vpool), pos, sh.L, sh.Hkv, sh.r,
@@ -866,6 +1055,17 @@ hipError_t launch_evict(const Shape& sh, const SeqMeta* meta, void* kpool,
                         hipStream_t s, int32_t* drops_out, int drop_stride) {
   if (slot_hi <= slot_lo) return hipSuccess;
   const int n_chunks = positions_only ? 0 : event_chunks(sh, max_candidates);
+  if (sh.dtype == 2 && !positions_only) {
+    if (sh.layout == 1) return hipErrorInvalidValue;
+    const hipError_t e = launch_mode<true>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi,
+                                           max_candidates, s, nullptr, 0, true);
+    if (e != hipSuccess) return e;
+    if (sh.layout == 2)
+      launch_move_e4m3<true>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, n_chunks, s);
+    else
+      launch_move_e4m3<false>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, n_chunks, s);
+    return hipGetLastError();
+  }
   if (n_chunks > 0) {
     const hipError_t e = launch_mode<true>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi,
                                            max_candidates, s, nullptr, 0, true);

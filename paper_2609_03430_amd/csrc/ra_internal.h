@@ -7,6 +7,7 @@
 //                                     one channel (the MFMA operand shape of
 //                                     the P.V product)
 //   pos     [pool_rows]               int32 token position of each row
+// In an e4m3 cache each pool is followed by [pool_rows] scale bytes (e4m3.h).
 // Contiguous layouts: a sequence owns L * Hkv consecutive regions of `cap`
 // rows (cap a multiple of 32); region (l, g) starts at row base + (l * Hkv +
 // g) * cap.  Rows [0, len) of a region are cached, in chronological order
@@ -72,7 +73,7 @@ struct DueList {
 };
 
 struct Shape {
-  int L, Hq, Hkv, G, r, every, dtype;  // dtype: 0 f32, 1 bf16
+  int L, Hq, Hkv, G, r, every, dtype;  // dtype: 0 f32, 1 bf16, 2 e4m3 (bf16 in and out)
   int layout;                          // 0 chronological, 1 hole-fill, 2 paged
   int policy;                          // ra_policy
   int block;                           // tokens per block (block policy)
@@ -84,6 +85,9 @@ struct Shape {
   int64_t move_words = 0;
   // the active sequences' rows fit the last-level cache between two events
   bool cached = false;
+  // e4m3 pools: the rows' scale bytes (e4m3.h)
+  uint8_t* k_scale = nullptr;
+  uint8_t* v_scale = nullptr;
 };
 
 // Pool row of row j of one (sequence, layer, KV head) cache.
@@ -131,7 +135,7 @@ hipError_t launch_evict(const Shape& sh, const SeqMeta* meta, void* kpool,
 // Workgroups per head of a full event's moves: one per chunk of rows, launched
 // after the selection (0: the workgroup that selects a head moves it, in one
 // launch).  A head's moved rows lie in [prompt, prompt + candidates + recent).
-constexpr int event_chunk_rows(int dtype) { return dtype == 1 ? 512 : 256; }
+constexpr int event_chunk_rows(int dtype) { return dtype == 0 ? 256 : 512; }
 constexpr int kMaxChunks = 21;   // bits of a head's sync word left for its chunks
 inline int event_chunks(const Shape& sh, int max_candidates) {
   if (!sh.move_sync || !sh.due || sh.due->n == 0 || sh.layout == 1) return 0;
@@ -155,6 +159,8 @@ inline int event_chunks(const Shape& sh, int max_candidates) {
   // 92).
   const int64_t moved = static_cast<int64_t>(max_candidates) + sh.r;
   const int n = static_cast<int>((moved + 7 + chunk - 1) / chunk);
+  if (sh.dtype == 2)   // the moves are a second launch either way (evict.hip)
+    return n > 1 && n <= kMaxChunks && heads * n <= 1024 ? n : 0;
   const int quarters = sh.dtype == 0 ? 7 : !sh.cached ? 6 : sh.every < 48 ? 9 : 7;
   if (4 * moved <= quarters * chunk || n > kMaxChunks || heads >= 128) return 0;
   const int rounds_from = !sh.cached ? 4 : sh.dtype == 0 ? 6 : kMaxChunks + 1;
@@ -189,6 +195,10 @@ hipError_t launch_write_rows(const Shape& sh, const SeqMeta& M, int slot, int le
 hipError_t launch_read_rows(const Shape& sh, const SeqMeta& M, int slot, int lg, int len,
                             const void* kpool, const void* vpool, void* k_out,
                             void* v_out, hipStream_t s);
+// Rows [0, len) of every head of slot `slot` to row-major outputs [L * Hkv][len][128].
+hipError_t launch_export_rows(const Shape& sh, const SeqMeta& M, int slot, int len,
+                              const void* kpool, const void* vpool, void* k_out, void* v_out,
+                              hipStream_t s);
 // Positions of rows [0, len) of every head of slot `slot`: [L * Hkv][len].
 hipError_t launch_export_positions(const Shape& sh, const SeqMeta& M, int slot, int len,
                                    const int32_t* pos, int32_t* out, hipStream_t s);
@@ -231,6 +241,49 @@ struct AttnLaunch {
   int* arrivals;
 };
 hipError_t launch_attention(const Shape& sh, const AttnLaunch& a, hipStream_t s);
+
+// Rows of a block-sparse step (blocks.hip): of a head of `len` cached rows, blocks
+// of kBlockRows rows below row kBlockRows * candidates are chosen from, later rows
+// and the step's new one always attended.
+constexpr int kBlockRows = 32;
+constexpr int kMaxBlocks = 16384;   // candidate blocks per head that are chosen from
+struct BlockChoice {
+  const int32_t* list;   // [slots][Hkv][stride] chosen blocks, ascending
+  int stride;
+  int n_blocks;          // blocks chosen per head where there are more candidates
+  int recent;            // most recent cached rows that are no candidates
+};
+__device__ __host__ inline int candidate_blocks(int len, int recent) {
+  return len > recent ? (len - recent) / kBlockRows : 0;
+}
+// The blocks that a step attends to are numbered 0 .. attended_blocks - 1: the
+// chosen ones, then those past the candidates, the last holding the new row.
+__device__ __host__ inline int attended_blocks(int len, int recent, int n_blocks) {
+  const int cand = candidate_blocks(len, recent);
+  return len / kBlockRows + 1 - (cand > n_blocks ? cand - n_blocks : 0);
+}
+// Bounds of the blocks' keys: kBoundsBytes int8 per block of the pool (the upper
+// bound of each channel, then the lower), then an int8 exponent per block.
+constexpr int kBoundsBytes = 2 * kHeadDim;
+struct BoundsRange {
+  int32_t slot, from, to;   // a slot's blocks [from, to) of every head of a layer
+};
+constexpr int kBoundsBatch = 64;   // ranges per launch
+hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void* kpool,
+                               int8_t* bounds, int64_t pool_rows, int layer,
+                               const BoundsRange* ranges, int n, hipStream_t s);
+// Chosen blocks of every head of the active slots below max_seqs that have more than
+// choice.n_blocks candidates, at most max_candidates, into `list` (choice.stride
+// per head).
+hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q,
+                                const int8_t* bounds, int64_t pool_rows, int layer, int max_seqs,
+                                const BlockChoice& choice, int32_t* list, int max_candidates,
+                                hipStream_t s);
+// Attention over the e4m3 rows of a cache, or with `choice` over the rows of a
+// block-sparse step (bf16 or e4m3).  a.split_keys counts attended rows.
+hipError_t launch_attention_e4m3(const Shape& sh, const AttnLaunch& a, hipStream_t s);
+hipError_t launch_block_attention(const Shape& sh, const AttnLaunch& a, const BlockChoice& choice,
+                                  hipStream_t s);
 
 // The allocation-free attention's partials: a file-scope device array of
 // kNoAllocScratchBytes (attention.hip).  scratch_address returns its device

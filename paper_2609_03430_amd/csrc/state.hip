@@ -6,6 +6,7 @@
 // steps, once the evictable rows exceed the budget) by writing an eviction
 // plan that the eviction kernel consumes.  The host library replays the
 // same integer rules on its mirror to decide which launches to issue.
+#include "e4m3.h"
 #include "ra_internal.h"
 
 namespace ra {
@@ -161,11 +162,11 @@ __global__ void write_rows_kernel(SeqMeta M, int slot, int len, Paging pg,
   }
 }
 
-// Rows [0, len) of one head to row-major outputs.  Grid: (ceil(len/32), 2): keys,
-// values; 128 threads.  One head is a short copy (1.6 MB at 3,136 bf16 rows), so its time
-// is the latency of a load and a store: every thread issues all its loads
-// before its stores, in 16-byte units (outputs are 16-byte aligned, as all
-// device pointers of the interface).  A thread takes kEpu channels x kEpu rows
+// Rows [0, len) of heads lg, lg + 1, .. to row-major outputs [heads][len][128].
+// Grid: (ceil(len/32), 2, heads): keys, values; 128 threads.  One head is a short
+// copy (1.6 MB at 3,136 bf16 rows), so its time is the latency of a load and a
+// store: every thread issues all its loads before its stores, in 16-byte units
+// (outputs are 16-byte aligned, as all device pointers of the interface).  A thread takes kEpu channels x kEpu rows
 // of a value tile and transposes them in registers.  Element by element it
 // took 23 us per 3,136-row head, in 16-byte units 5.5, keys and values side by
 // side 4.5.
@@ -179,14 +180,15 @@ __global__ __launch_bounds__(128) void read_rows_kernel(SeqMeta M, int slot, int
   constexpr int kEpu = 16 / sizeof(E);
   constexpr int kUnitsRow = kHeadDim / kEpu;
   constexpr int kPer = kReadRows * kUnitsRow / 128;       // key units per thread
-  const RowMap rm = row_map(M, slot, lg, pg);
+  const RowMap rm = row_map(M, slot, lg + blockIdx.z, pg);
+  const int64_t out0 = static_cast<int64_t>(blockIdx.z) * len;
   const int j0 = blockIdx.x * kReadRows;                  // 32 rows lie in one page
   const int64_t row0 = pool_row<PAGED>(rm, j0);
   if (blockIdx.y == 0) {
     if (!k_out) return;
     u32x4 k[kPer];
     const u32x4* src = reinterpret_cast<const u32x4*>(kpool + row0 * kHeadDim);
-    u32x4* dst = reinterpret_cast<u32x4*>(k_out + static_cast<int64_t>(j0) * kHeadDim);
+    u32x4* dst = reinterpret_cast<u32x4*>(k_out + (out0 + j0) * kHeadDim);
     const int n = min(kReadRows, len - j0) * kUnitsRow;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -220,8 +222,164 @@ __global__ __launch_bounds__(128) void read_rows_kernel(SeqMeta M, int slot, int
       u32x4 x;
       __builtin_memcpy(&x, out, 16);
       if (j + e < len)
-        *reinterpret_cast<u32x4*>(v_out + static_cast<int64_t>(j + e) * kHeadDim + ch) = x;
+        *reinterpret_cast<u32x4*>(v_out + (out0 + j + e) * kHeadDim + ch) = x;
     }
+  }
+}
+
+// ---- e4m3 rows (e4m3.h) ------------------------------------------------------------
+
+// Sixteen lanes take an 8-row tile of keys or of values, eight channels each: the
+// largest magnitude of a row is joined over the sixteen lanes, and the codes are
+// packed two at a time in the order in which they are stored, along the channels
+// for keys and along the rows for values, so that the transposition costs nothing.
+// Bound by HBM: 256 B read and 129 written per row.
+constexpr int kTileLanes = 16;
+constexpr int kQuantRows = 256 / kTileLanes * 8;   // rows per workgroup of 256 threads
+
+// Row-major bf16 rows [L * Hkv][len][128] into rows [0, len) of each head.
+// Grid: (ceil(len / 128), L * Hkv, 2): keys (and positions), values.
+template <bool PAGED>
+__global__ __launch_bounds__(256) void write_rows_e4m3_kernel(
+    SeqMeta M, int slot, int len, Paging pg, const uint16_t* __restrict__ k_src,
+    const uint16_t* __restrict__ v_src, const int32_t* __restrict__ pos_src,
+    uint8_t* __restrict__ kpool, uint8_t* __restrict__ vpool, uint8_t* __restrict__ kscale,
+    uint8_t* __restrict__ vscale, int32_t* __restrict__ pos) {
+  const int lg = blockIdx.y;
+  const bool keys = blockIdx.z == 0;
+  const RowMap rm = row_map(M, slot, lg, pg);
+  const int64_t src0 = static_cast<int64_t>(lg) * len;
+  if (pos && keys) {
+    for (int i = threadIdx.x; i < kQuantRows; i += 256) {
+      const int j = static_cast<int>(blockIdx.x) * kQuantRows + i;
+      if (j < len) pos[pool_row<PAGED>(rm, j)] = pos_src ? pos_src[src0 + j] : j;
+    }
+  }
+  const uint16_t* src = keys ? k_src : v_src;
+  if (!src) return;
+  const int c8 = threadIdx.x % kTileLanes;
+  const int jt = static_cast<int>(blockIdx.x) * kQuantRows + threadIdx.x / kTileLanes * 8;
+  if (jt >= len) return;                       // (all sixteen lanes of the tile)
+  src += (src0 + jt) * kHeadDim + 8 * c8;
+  u32x4 in[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    in[e] = u32x4{0u, 0u, 0u, 0u};
+    if (jt + e < len) in[e] = *reinterpret_cast<const u32x4*>(src + e * kHeadDim);
+  }
+  uint64_t scales = 0;
+  float x[8][8];                               // [row][channel], divided by the row's scale
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[e][2 * i] = bf16_low(in[e][i]);
+      x[e][2 * i + 1] = bf16_high(in[e][i]);
+      amax = max(amax, max(row_magnitude(x[e][2 * i]), row_magnitude(x[e][2 * i + 1])));
+    }
+#pragma unroll
+    for (int o = 1; o < kTileLanes; o <<= 1)
+      amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
+    const uint32_t byte = e4m3_scale_byte(amax);
+    scales |= static_cast<uint64_t>(byte) << (8 * e);
+    const float inv = e4m3_inverse(byte);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[e][c] = e4m3_clamp(x[e][c] * inv, byte);
+  }
+  const int64_t row0 = pool_row<PAGED>(rm, jt);          // a tile lies in one page
+  if (c8 == 0) *reinterpret_cast<uint64_t*>((keys ? kscale : vscale) + row0) = scales;
+  const auto pack4 = [](float a, float b, float c, float d) {
+    return e4m3_pack2<true>(c, d, e4m3_pack2<false>(a, b, 0u));
+  };
+  if (keys) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (jt + e < len) {
+        uint2 w;
+        w.x = pack4(x[e][0], x[e][1], x[e][2], x[e][3]);
+        w.y = pack4(x[e][4], x[e][5], x[e][6], x[e][7]);
+        *reinterpret_cast<uint2*>(kpool + (row0 + e) * kHeadDim + 8 * c8) = w;
+      }
+    }
+    return;
+  }
+  uint8_t* dst = vpool + row0 * kHeadDim + 64 * c8;       // rows past len are zero codes
+#pragma unroll
+  for (int c = 0; c < 8; c += 2) {
+    u32x4 w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[2 * h] = pack4(x[0][c + h], x[1][c + h], x[2][c + h], x[3][c + h]);
+      w[2 * h + 1] = pack4(x[4][c + h], x[5][c + h], x[6][c + h], x[7][c + h]);
+    }
+    *reinterpret_cast<u32x4*>(dst + 8 * c) = w;
+  }
+}
+
+// Rows [0, len) of heads lg, lg + 1, .. to row-major bf16 outputs [heads][len][128],
+// the values that the rows stand for.  Grid: (ceil(len / 128), 2, heads).
+template <bool PAGED>
+__global__ __launch_bounds__(256) void read_rows_e4m3_kernel(
+    SeqMeta M, int slot, int lg, int len, Paging pg, const uint8_t* __restrict__ kpool,
+    const uint8_t* __restrict__ vpool, const uint8_t* __restrict__ kscale,
+    const uint8_t* __restrict__ vscale, uint16_t* __restrict__ k_out,
+    uint16_t* __restrict__ v_out) {
+  const bool keys = blockIdx.y == 0;
+  uint16_t* out = keys ? k_out : v_out;
+  const int c8 = threadIdx.x % kTileLanes;
+  const int jt = static_cast<int>(blockIdx.x) * kQuantRows + threadIdx.x / kTileLanes * 8;
+  if (!out || jt >= len) return;
+  const RowMap rm = row_map(M, slot, lg + blockIdx.z, pg);
+  const int64_t row0 = pool_row<PAGED>(rm, jt);
+  out += (static_cast<int64_t>(blockIdx.z) * len + jt) * kHeadDim + 8 * c8;
+  const uint64_t scales = *reinterpret_cast<const uint64_t*>((keys ? kscale : vscale) + row0);
+  const auto scale_of = [&](int e) {
+    return e4m3_scale(static_cast<uint32_t>(scales >> (8 * e)) & 255u);
+  };
+  if (keys) {
+    uint2 w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (jt + e < len)
+        w[e] = *reinterpret_cast<const uint2*>(kpool + (row0 + e) * kHeadDim + 8 * c8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (jt + e >= len) continue;
+      const float s = scale_of(e);
+      u32x4 o;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t c = i ? w[e].y : w[e].x;
+        const f32x2 a = e4m3_unpack2<false>(c), b = e4m3_unpack2<true>(c);
+        o[2 * i] = bf16_pack_exact(a[0] * s, a[1] * s);
+        o[2 * i + 1] = bf16_pack_exact(b[0] * s, b[1] * s);
+      }
+      *reinterpret_cast<u32x4*>(out + e * kHeadDim) = o;
+    }
+    return;
+  }
+  u32x4 w[4];                                  // two channels of eight rows each
+  const u32x4* src = reinterpret_cast<const u32x4*>(vpool + row0 * kHeadDim + 64 * c8);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = src[i];
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float s0 = scale_of(e), s1 = scale_of(e + 1);
+    f32x2 x[8];                                // rows e, e + 1 of the eight channels
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t word = w[c / 2][c % 2 * 2 + e / 4];
+      x[c] = e & 2 ? e4m3_unpack2<true>(word) : e4m3_unpack2<false>(word);
+    }
+    u32x4 a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = bf16_pack_exact(x[2 * i][0] * s0, x[2 * i + 1][0] * s0);
+      b[i] = bf16_pack_exact(x[2 * i][1] * s1, x[2 * i + 1][1] * s1);
+    }
+    if (jt + e < len) *reinterpret_cast<u32x4*>(out + e * kHeadDim) = a;
+    if (jt + e + 1 < len) *reinterpret_cast<u32x4*>(out + (e + 1) * kHeadDim) = b;
   }
 }
 
@@ -321,12 +479,25 @@ void write_rows_t(const Shape& sh, const SeqMeta& M, int slot, int len, const vo
                        pos);
 }
 
+void write_rows_e4m3(const Shape& sh, const SeqMeta& M, int slot, int len, const void* k_src,
+                     const void* v_src, const int32_t* pos_src, void* kpool, void* vpool,
+                     int32_t* pos, hipStream_t s) {
+  const dim3 grid((len + kQuantRows - 1) / kQuantRows, sh.L * sh.Hkv, 2);
+  const auto kernel = sh.pg.tables ? write_rows_e4m3_kernel<true> : write_rows_e4m3_kernel<false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, M, slot, len, sh.pg,
+                     static_cast<const uint16_t*>(k_src), static_cast<const uint16_t*>(v_src),
+                     pos_src, static_cast<uint8_t*>(kpool), static_cast<uint8_t*>(vpool),
+                     sh.k_scale, sh.v_scale, pos);
+}
+
 hipError_t launch_write_rows(const Shape& sh, const SeqMeta& M, int slot, int len,
                              const void* k_src, const void* v_src,
                              const int32_t* pos_src, void* kpool, void* vpool,
                              int32_t* pos, hipStream_t s) {
   if (len <= 0) return hipSuccess;
-  if (sh.dtype == 1)
+  if (sh.dtype == 2)
+    write_rows_e4m3(sh, M, slot, len, k_src, v_src, pos_src, kpool, vpool, pos, s);
+  else if (sh.dtype == 1)
     write_rows_t<uint16_t>(sh, M, slot, len, k_src, v_src, pos_src, kpool, vpool, pos, s);
   else
     write_rows_t<float>(sh, M, slot, len, k_src, v_src, pos_src, kpool, vpool, pos, s);
@@ -334,10 +505,10 @@ hipError_t launch_write_rows(const Shape& sh, const SeqMeta& M, int slot, int le
 }
 
 template <typename E>
-void read_rows_t(const Shape& sh, const SeqMeta& M, int slot, int lg, int len,
+void read_rows_t(const Shape& sh, const SeqMeta& M, int slot, int lg, int heads, int len,
                  const void* kpool, const void* vpool, void* k_out, void* v_out,
                  hipStream_t s) {
-  const dim3 grid((len + kReadRows - 1) / kReadRows, 2);
+  const dim3 grid((len + kReadRows - 1) / kReadRows, 2, heads);
   const E* k = static_cast<const E*>(kpool);
   const E* v = static_cast<const E*>(vpool);
   if (sh.pg.tables)
@@ -348,15 +519,46 @@ void read_rows_t(const Shape& sh, const SeqMeta& M, int slot, int lg, int len,
                        sh.pg, k, v, static_cast<E*>(k_out), static_cast<E*>(v_out));
 }
 
+// Heads lg .. lg + heads - 1 (at most 65,535 of them: a grid's z).
+hipError_t read_heads(const Shape& sh, const SeqMeta& M, int slot, int lg, int heads, int len,
+                      const void* kpool, const void* vpool, void* k_out, void* v_out,
+                      hipStream_t s) {
+  if (len <= 0) return hipSuccess;
+  if (sh.dtype == 2) {
+    const dim3 grid((len + kQuantRows - 1) / kQuantRows, 2, heads);
+    const auto kernel = sh.pg.tables ? read_rows_e4m3_kernel<true> : read_rows_e4m3_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, M, slot, lg, len, sh.pg,
+                       static_cast<const uint8_t*>(kpool), static_cast<const uint8_t*>(vpool),
+                       sh.k_scale, sh.v_scale, static_cast<uint16_t*>(k_out),
+                       static_cast<uint16_t*>(v_out));
+  } else if (sh.dtype == 1) {
+    read_rows_t<uint16_t>(sh, M, slot, lg, heads, len, kpool, vpool, k_out, v_out, s);
+  } else {
+    read_rows_t<float>(sh, M, slot, lg, heads, len, kpool, vpool, k_out, v_out, s);
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_read_rows(const Shape& sh, const SeqMeta& M, int slot, int lg, int len,
                             const void* kpool, const void* vpool, void* k_out,
                             void* v_out, hipStream_t s) {
-  if (len <= 0) return hipSuccess;
-  if (sh.dtype == 1)
-    read_rows_t<uint16_t>(sh, M, slot, lg, len, kpool, vpool, k_out, v_out, s);
-  else
-    read_rows_t<float>(sh, M, slot, lg, len, kpool, vpool, k_out, v_out, s);
-  return hipGetLastError();
+  return read_heads(sh, M, slot, lg, 1, len, kpool, vpool, k_out, v_out, s);
+}
+
+hipError_t launch_export_rows(const Shape& sh, const SeqMeta& M, int slot, int len,
+                              const void* kpool, const void* vpool, void* k_out, void* v_out,
+                              hipStream_t s) {
+  constexpr int kMost = 32768;
+  const size_t head_bytes = static_cast<size_t>(len) * kHeadDim * (sh.dtype == 0 ? 4 : 2);
+  for (int lg = 0; lg < sh.L * sh.Hkv; lg += kMost) {
+    const auto at = [&](void* p) {
+      return p ? static_cast<void*>(static_cast<char*>(p) + lg * head_bytes) : nullptr;
+    };
+    const hipError_t e = read_heads(sh, M, slot, lg, std::min(kMost, sh.L * sh.Hkv - lg), len,
+                                    kpool, vpool, at(k_out), at(v_out), s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_export_positions(const Shape& sh, const SeqMeta& M, int slot, int len,
