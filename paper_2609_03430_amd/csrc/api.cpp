@@ -278,12 +278,13 @@ int mid_plan(const ra_cache* c, Plan& p, int heads, int keys_max, int64_t keys_m
 Plan ra::host::plan_blocks(const ra_cache* c, int64_t keys_max, int heads) {
   Plan p;
   p.waves = 4;
-  const int unit = 32 * p.waves;
+  const int unit = 2 * 32 * p.waves;
   const int64_t splits =
-      std::min<int64_t>(ra::kMaxSplits, heads >= 768 ? 1 : (512 + heads - 1) / heads);
-  int64_t sk = c->cfg.attn_split > 0 ? c->cfg.attn_split : (keys_max + splits - 1) / splits;
+      std::min<int64_t>(ra::kMaxSplits, std::max(1, (256 + heads / 2) / heads));
+  int64_t sk = c->cfg.attn_split > 0 ? c->cfg.attn_split
+                                     : std::max<int64_t>(unit, (keys_max + splits - 1) / splits);
   sk = std::max(sk, (keys_max + ra::kMaxSplits - 1) / ra::kMaxSplits);
-  p.split_keys = static_cast<int>(round_up(sk, unit));
+  p.split_keys = static_cast<int>(round_up(sk, 32));
   p.max_splits = p.partials = static_cast<int>((keys_max + p.split_keys - 1) / p.split_keys);
   p.whole = p.max_splits == 1;
   return p;

@@ -23,6 +23,11 @@ size_t list_bytes(const ra_config& c, int32_t n_blocks) {
   return (n + 255) / 256 * 256;
 }
 
+// Scores of the candidates, which the attention's partials follow in the same place.
+size_t scores_bytes(const ra_config& c) {
+  return static_cast<size_t>(c.max_seqs) * c.num_kv_heads * ra::kMaxBlocks * sizeof(uint32_t);
+}
+
 }  // namespace
 
 extern "C" {
@@ -54,7 +59,7 @@ size_t ra_sparse_bytes(const ra_config* c, int64_t pool_rows) {
 
 size_t ra_sparse_workspace_bytes(const ra_config* c, int32_t n_blocks) {
   if (ra_config_check(c) != RA_OK || !sparse_supported(*c) || n_blocks < 0) return 0;
-  return ra_workspace_bytes(c) + list_bytes(*c, n_blocks);
+  return list_bytes(*c, n_blocks) + std::max(ra_workspace_bytes(c), scores_bytes(*c));
 }
 
 ra_status ra_sparse_attach(ra_cache* c, void* bounds, size_t bounds_bytes, void* stream) {
@@ -109,10 +114,12 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
       c->bounds_built[static_cast<size_t>(layer) * c->cfg.max_seqs + r.slot] = r.to;
   }
   int32_t* list = static_cast<int32_t*>(workspace);
+  void* scratch = static_cast<char*>(workspace) + list_bytes(c->cfg, n_blocks);
   const ra::BlockChoice choice{list, std::min(n_blocks, ra::kMaxBlocks), n_blocks, recent_rows};
   if (candidates > 0 && n_blocks > 0)
     RA_LAUNCH(ra::launch_choose_blocks(sh, c->meta, q, c->bounds, c->pool_rows, layer, c->slot_hi,
-                                       choice, list, candidates, hs));
+                                       choice, list, static_cast<uint32_t*>(scratch),
+                                       ra::kMaxBlocks, c->arrivals, candidates, hs));
   c->appended[layer] = 1;
   ++c->n_appended;
   if (n_active == 0) return RA_OK;
@@ -128,7 +135,7 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
   a.k_new = k_new;
   a.v_new = v_new;
   a.out = out;
-  a.ws_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + list_bytes(c->cfg, n_blocks));
+  a.ws_o = static_cast<float*>(scratch);
   a.ws_ml = a.ws_o + items * c->G * ra::kHeadDim;
   a.split_stride = ra::kMaxSplits;
   a.layer = layer;

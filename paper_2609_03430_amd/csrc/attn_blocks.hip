@@ -70,20 +70,40 @@ struct Pools {
   const uint8_t* v_scale;
 };
 
+// The largest of the lanes with the same lane & 15, in registers: the two rows of 16
+// lanes of each half exchanged, then the halves.
+__device__ __forceinline__ float max_over_groups(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// 2^x, a result below 2^-126 flushed to zero: nothing beside a weight of 1.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
 // ---- bf16 rows -----------------------------------------------------------------
 
 struct Bf16Rows {
   using Block = BlockRegs;
   using Channels = RowChannels;
-  using Query = bf16x8[4];
+  struct Query {
+    bf16x8 q[4];
+    __device__ __forceinline__ void load(const uint16_t* row, bool real, int grp) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const u32x4 z = {0u, 0u, 0u, 0u};
+        const u32x4 x = ld16(row + 32 * s + 8 * grp);
+        q[s] = as_bf16x8(real ? x : z);
+      }
+    }
+  };
 
   static __device__ __forceinline__ void load(Block& b, const Pools& p, int64_t row,
                                               const LaneMap& lm) {
     load_block(b, static_cast<const uint16_t*>(p.k) + row * kHeadDim,
                static_cast<const uint16_t*>(p.v) + row * kHeadDim, 0, lm);
-  }
-  static __device__ __forceinline__ int query_channel(int step, int grp) {
-    return 32 * step + 8 * grp;
   }
   // The step's pair, as bf16 in LDS (called by one whole wavefront).
   struct New {
@@ -125,22 +145,25 @@ struct Bf16Rows {
       }
     }
   };
-  static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const bf16x8 (&q)[4],
+  static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const Query& q,
                                                  float scale_log2, int limit) {
-    compute_block(st, b, q, scale_log2, limit);
+    compute_block(st, b, q.q, scale_log2, limit);
   }
 };
 
 // ---- e4m3 rows -------------------------------------------------------------------
 
-// A lane's 16-byte loads hold 16 channels of a key row, two k-steps' operands, and
-// two channels of a value tile, the operands of two output tiles: output tile 2u + h
-// is channels 32u + 2 * (its row) + h.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// A lane's 16-byte loads hold 16 channels of a key row, and two channels of a value
+// tile, the operands of two output tiles: output tile 2u + h is channels 32u + 2 *
+// (its row) + h.
 struct E4m3Block {
   u32x4 k[2][2];     // [S tile][64 channels]
   u32x4 v[4];        // [32 channels]
   uint64_t vs;       // scale bytes of the lane's eight values' rows
-  uint32_t ks[2];    // scale bytes of its two key rows
+  uint64_t ks;       // .. of eight key rows, its two among them (key_byte, + 4)
 };
 
 struct E4m3Rows {
@@ -151,25 +174,71 @@ struct E4m3Rows {
     }
   };
 
+  // S^T comes from the codes themselves (v_mfma_scale_f32_16x16x128_f8f6f4, the rows'
+  // scale bytes its operands' scales), so the query has to be in 8 bits too: it is
+  // the sum of two E4M3 rows, hi = E4M3(q / 2^s) and lo = E4M3(16 (q / 2^s - hi)).
+  // A bf16 value has 8 significant bits, hi the first four and lo the others, so the
+  // sum is exact where |q_c| is at least 2^-14 of the row's largest, and below it is
+  // off by at most 2^-22 of the largest: the size of the products' fp32 rounding.
+  // (16 products of 16x16x128 per 128 keys, where converting the keys to bf16 took as
+  // many matrix cycles and 32 to 64 vector instructions per 32 keys.)
+  struct Query {
+    i32x8 hi, lo;
+    int scale_hi, scale_lo;
+    __device__ __forceinline__ void load(const uint16_t* row, bool real, int grp) {
+      float x[32];
+      uint32_t amax = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x4 w = ld16(row + 64 * (i >> 1) + 16 * grp + 8 * (i & 1));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t u = real ? w[j] : 0u;
+          x[8 * i + 2 * j] = bf16_low(u);
+          x[8 * i + 2 * j + 1] = bf16_high(u);
+          amax = max(amax, max(row_magnitude(bf16_low(u)), row_magnitude(bf16_high(u))));
+        }
+      }
+#pragma unroll
+      for (int o = 16; o < 64; o <<= 1)
+        amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
+      const uint32_t byte = max(e4m3_scale_byte(amax), 5u);     // lo's is four less
+      const float inv = e4m3_inverse(byte);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = e4m3_clamp(x[i] * inv, byte);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t h = e4m3_pack2<true>(x[4 * i + 2], x[4 * i + 3],
+                                            e4m3_pack2<false>(x[4 * i], x[4 * i + 1], 0u));
+        const f32x2 a = e4m3_unpack2<false>(h), b = e4m3_unpack2<true>(h);
+        const uint32_t l = e4m3_pack2<true>(
+            16.f * (x[4 * i + 2] - b[0]), 16.f * (x[4 * i + 3] - b[1]),
+            e4m3_pack2<false>(16.f * (x[4 * i] - a[0]), 16.f * (x[4 * i + 1] - a[1]), 0u));
+        hi[i] = static_cast<int>(h);
+        lo[i] = static_cast<int>(l);
+      }
+      scale_hi = static_cast<int>(byte);
+      scale_lo = static_cast<int>(byte - 4);
+    }
+  };
+
+  // bit of a lane's first key row's byte in Block::ks
+  static __device__ __forceinline__ int key_shift() { return 8 * (threadIdx.x & 3); }
+
   static __device__ __forceinline__ void load(Block& b, const Pools& p, int64_t row,
                                               const LaneMap& lm) {
     const uint8_t* K = static_cast<const uint8_t*>(p.k) + row * kHeadDim;
     const uint8_t* V = static_cast<const uint8_t*>(p.v) + row * kHeadDim;
+    b.ks = *reinterpret_cast<const uint64_t*>(p.k_scale + row + (lm.krow[0] & ~7));
+    b.vs = *reinterpret_cast<const uint64_t*>(p.v_scale + row + lm.vrow);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      b.ks[t] = p.k_scale[row + lm.krow[t]];
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         b.k[t][s] = ld16(K + lm.krow[t] * kHeadDim + 2 * lm.kcol + 64 * s);
-    }
-    b.vs = *reinterpret_cast<const uint64_t*>(p.v_scale + row + lm.vrow);
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       b.v[u] = ld16_stream(V + lm.vrow * kHeadDim + (32 * u + 2 * lm.vch) * 8);
-  }
-  // first channel of a lane's operand at k-step `step`
-  static __device__ __forceinline__ int query_channel(int step, int grp) {
-    return 64 * (step >> 1) + 16 * grp + 8 * (step & 1);
   }
 
   struct New {
@@ -204,7 +273,8 @@ struct E4m3Rows {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
         if (lm.krow[t] == at) {
-          b.ks[t] = ks;
+          const int bit = key_shift() + 32 * t;
+          b.ks = (b.ks & ~(uint64_t(255) << bit)) | static_cast<uint64_t>(ks) << bit;
 #pragma unroll
           for (int s = 0; s < 2; ++s) b.k[t][s] = ld16(k + 2 * lm.kcol + 64 * s);
         }
@@ -242,33 +312,34 @@ struct E4m3Rows {
     }
   };
 
-  // Eight codes of one scale to the bf16 numbers that they stand for (exact).
-  static __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale) {
-    const f32x2 a = e4m3_unpack2<false>(w0), b = e4m3_unpack2<true>(w0);
-    const f32x2 c = e4m3_unpack2<false>(w1), d = e4m3_unpack2<true>(w1);
-    u32x4 r;
-    r.x = bf16_pack_exact(a[0] * scale, a[1] * scale);
-    r.y = bf16_pack_exact(b[0] * scale, b[1] * scale);
-    r.z = bf16_pack_exact(c[0] * scale, c[1] * scale);
-    r.w = bf16_pack_exact(d[0] * scale, d[1] * scale);
-    return as_bf16x8(r);
+  // Eight codes as bf16 numbers.
+  static __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1) {
+    union {
+      bf16x2 h[4];
+      bf16x8 v;
+    } r;
+    r.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false);
+    r.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true);
+    r.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false);
+    r.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true);
+    return r.v;
   }
 
   // compute_block over the values that the rows stand for: a key's scale goes with
   // its codes, a value's with its weight.
-  static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const bf16x8 (&q)[4],
+  static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const Query& q,
                                                  float scale_log2, int limit) {
-    f32x4 s[2] = {};
+    f32x4 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const float scale = e4m3_scale(b.ks[t]);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(b.k[t][i].x, b.k[t][i].y, scale),
-                                                       q[2 * i], s[t], 0, 0, 0);
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16(b.k[t][i].z, b.k[t][i].w, scale),
-                                                       q[2 * i + 1], s[t], 0, 0, 0);
-      }
+      const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+      i32x8 k;
+      __builtin_memcpy(&k, b.k[t], 32);
+      const int scale = static_cast<int>(static_cast<uint32_t>(b.ks >> (32 * t)) >> key_shift());
+      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.lo, z, 0, 0, 0, scale, 0,
+                                                              q.scale_lo);
+      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.hi, s[t], 0, 0, 0, scale, 0,
+                                                              q.scale_hi);
     }
     const int grp = (threadIdx.x & 63) >> 4;
     float x[8];
@@ -285,16 +356,16 @@ struct E4m3Rows {
     float bm = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
-    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
-    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-    const float mn = fmaxf(st.m, bm);
-    const float alpha = exp2f(st.m - mn);
+    const float mn = fmaxf(st.m, max_over_groups(bm));
+    const float alpha = exp2_fast(st.m - mn);
+    // weights times their values' scales as hi + lo, both bf16 (16 significant bits)
     bf16x8 p_hi, p_lo;
     float psum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float pf = exp2f(x[e] - mn);
-      const float pv = pf * e4m3_scale(static_cast<uint32_t>(b.vs >> (8 * e)) & 255u);
+      const float pf = exp2_fast(x[e] - mn);
+      const uint32_t w = static_cast<uint32_t>(b.vs >> (32 * (e >> 2)));
+      const float pv = pf * e4m3_scale(w >> (8 * (e & 3)) & 255u);
       const __bf16 hi = static_cast<__bf16>(pv);
       p_hi[e] = hi;
       p_lo[e] = static_cast<__bf16>(pv - static_cast<float>(hi));
@@ -305,7 +376,7 @@ struct E4m3Rows {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const u32x4 w = b.v[u >> 1];
-      const bf16x8 v = u & 1 ? to_bf16(w.z, w.w, 1.f) : to_bf16(w.x, w.y, 1.f);
+      const bf16x8 v = u & 1 ? to_bf16(w.z, w.w) : to_bf16(w.x, w.y);
       st.acc[u] *= alpha;
       st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_hi, st.acc[u], 0, 0, 0);
       st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_lo, st.acc[u], 0, 0, 0);
@@ -358,33 +429,31 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
 #pragma unroll
   for (int u = 0; u < 8; ++u) st.acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (has) {
-    bf16x8 qop[4];
-    const uint16_t* qrow = static_cast<const uint16_t*>(a.q) +
-                           (static_cast<int64_t>(w.slot) * Hq + w.g * G + (qi < G ? qi : 0)) * kHeadDim;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const u32x4 z = {0u, 0u, 0u, 0u};
-      const u32x4 x = ld16(qrow + R::query_channel(s, grp));
-      qop[s] = as_bf16x8(qi < G ? x : z);
-    }
+    const int last = b1 - 1;
+    typename R::Block x0, x1;
+    load(x0, b0);
+    load(x1, min(b0 + 1, last));
+    typename R::Query q;
+    q.load(static_cast<const uint16_t*>(a.q) +
+               (static_cast<int64_t>(w.slot) * Hq + w.g * G + (qi < G ? qi : 0)) * kHeadDim,
+           qi < G, grp);
     if (owns_last) {
       const int64_t src = (static_cast<int64_t>(w.slot) * Hkv + w.g) * kHeadDim;
       s_new.stage(static_cast<const uint16_t*>(a.k_new) + src,
                   static_cast<const uint16_t*>(a.v_new) + src);
     }
-    const int last = b1 - 1;
-    typename R::Block x0, x1;
-    load(x0, b0);
-    load(x1, min(b0 + 1, last));
+    // two register buffers in turn; every prefetch is issued (the last block's again
+    // once there is none left), so that the wait for a block leaves the next one's
+    // loads in flight
     int i = b0;
     for (; i + 1 < last; i += 2) {
-      R::compute(st, x0, qop, scale_log2, 32);
+      R::compute(st, x0, q, scale_log2, 32);
       load(x0, min(i + 2, last));
-      R::compute(st, x1, qop, scale_log2, 32);
+      R::compute(st, x1, q, scale_log2, 32);
       load(x1, min(i + 3, last));
     }
     if (i < last) {
-      R::compute(st, x0, qop, scale_log2, 32);
+      R::compute(st, x0, q, scale_log2, 32);
       x0 = x1;
     }
     int limit = 32;
@@ -393,7 +462,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
       s_new.patch(x0, at, lm);
       limit = at + 1;
     }
-    R::compute(st, x0, qop, scale_log2, limit);
+    R::compute(st, x0, q, scale_log2, limit);
     st.l += __shfl_xor(st.l, 16, 64);
     st.l += __shfl_xor(st.l, 32, 64);
   }
@@ -412,8 +481,8 @@ template <typename R, bool PAGED, bool LIST>
 void launch_blocks(const Shape& sh, const AttnLaunch& a, const BlockChoice& ch, hipStream_t s) {
   const dim3 grid(a.max_splits, sh.Hkv, a.max_seqs);
   const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(kHeadDim));
-  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, 1, PAGED, LIST>), grid, dim3(256), 0, s, a, ch,
-                     sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
+  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, 2, PAGED, LIST>), grid, dim3(256), 0, s,
+                     a, ch, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
 }
 
 }  // namespace

@@ -26,6 +26,22 @@ namespace ra {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// Exchanges within rows of 16 lanes that bring every lane together with the others:
+// neighbours, pairs, quads (mirrored) and eights (mirrored).
+template <typename F>
+__device__ __forceinline__ uint32_t over_row16(uint32_t x, F&& join) {
+#define RA_DPP(ctrl) \
+  static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), ctrl, 0xf, 0xf, false))
+  x = join(x, RA_DPP(0xB1));    // quad_perm [1, 0, 3, 2]
+  x = join(x, RA_DPP(0x4E));    // quad_perm [2, 3, 0, 1]
+  x = join(x, RA_DPP(0x141));   // row_half_mirror
+  return join(x, RA_DPP(0x140));   // row_mirror
+#undef RA_DPP
+}
+__device__ __forceinline__ uint32_t max_over_row16(uint32_t x) {
+  return over_row16(x, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+
 // |x| as the scale sees it (its bits).
 __device__ __forceinline__ uint32_t row_magnitude(float x) {
   const uint32_t b = __float_as_uint(x) & 0x7fffffffu;

@@ -274,10 +274,13 @@ hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void*
                                const BoundsRange* ranges, int n, hipStream_t s);
 // Chosen blocks of every head of the active slots below max_seqs that have more than
 // choice.n_blocks candidates, at most max_candidates, into `list` (choice.stride
-// per head).
+// per head).  Heads of several workgroups pass their scores through `scores`
+// (score_stride words per head) and count themselves on `arrivals`, a word per
+// (slot, KV head) that is zero between launches.
 hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q,
                                 const int8_t* bounds, int64_t pool_rows, int layer, int max_seqs,
-                                const BlockChoice& choice, int32_t* list, int max_candidates,
+                                const BlockChoice& choice, int32_t* list, uint32_t* scores,
+                                int score_stride, int* arrivals, int max_candidates,
                                 hipStream_t s);
 // Attention over the e4m3 rows of a cache, or with `choice` over the rows of a
 // block-sparse step (bf16 or e4m3).  a.split_keys counts attended rows.

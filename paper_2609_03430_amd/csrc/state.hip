@@ -278,10 +278,7 @@ __global__ __launch_bounds__(256) void write_rows_e4m3_kernel(
       x[e][2 * i + 1] = bf16_high(in[e][i]);
       amax = max(amax, max(row_magnitude(x[e][2 * i]), row_magnitude(x[e][2 * i + 1])));
     }
-#pragma unroll
-    for (int o = 1; o < kTileLanes; o <<= 1)
-      amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
-    const uint32_t byte = e4m3_scale_byte(amax);
+    const uint32_t byte = e4m3_scale_byte(max_over_row16(amax));
     scales |= static_cast<uint64_t>(byte) << (8 * e);
     const float inv = e4m3_inverse(byte);
 #pragma unroll
