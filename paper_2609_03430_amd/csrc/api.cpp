@@ -274,17 +274,41 @@ int mid_plan(const ra_cache* c, Plan& p, int heads, int keys_max, int64_t keys_m
 }  // namespace
 
 // Attention over blocks of rows (attn_blocks.hip): `heads` heads of up to keys_max
-// attended rows.
+// attended rows, workgroups of four wavefronts, three of which fit a CU.  Measured with
+// e4m3 rows and G = 5 (microseconds per step, splits of a head: time):
+//   up to 256 heads, as many splits as leave no CU two workgroups: 96 heads of 9,000 keys
+//     2: 46, 3: 59; 64 heads 4: 33, 8: 36; 192 heads 1: 84, 2: 96;
+//   no fewer than 256 keys to a workgroup (past 64 heads 512), half as many again
+//     staying whole: 8 heads of 300 keys 1: 7.5, 2: 8.4; of 2,200 9: 10.3, 14: 11.3; 128
+//     heads of 600 1: 13.4, 2: 14.6;
+//   past 12 splits the merge of one more costs 0.4, a workgroup 1,000 keys 5.7: 8 heads of
+//     9,000 keys 12: 14.4, 32: 17.2; of 30,000 12: 25.5, 24: 23.0, 32: 22.6;
+//   between 256 and 768 heads, long ones are split where that evens out the CUs' load:
+//     of 9,000 keys, 264 heads 1: 160, 2: 141, 3: 133, 6: 128; 320 1: 166, 2: 148, 3: 140;
+//     384 1: 178, 2: 162, 3: 168; 512 1: 208, 2: 211; 640 1: 276, 2: 265; of 2,200, 264
+//     heads 1: 47, 3: 44; 320 1: 50, 3: 52; 640 1: 88, 2: 95.
+// The partials of heads past 256 must fit the no-alloc entry point's array, which whole
+// heads do not need.
 Plan ra::host::plan_blocks(const ra_cache* c, int64_t keys_max, int heads) {
+  int64_t splits = 1;
+  const int64_t unit = heads > 64 ? 512 : 256;
+  if (heads <= 256) {
+    splits = 256 / heads;
+    if (splits > 12) splits = std::max<int64_t>(12, std::min(splits, keys_max / 1000));
+  } else if (keys_max >= 4096) {
+    splits = heads <= 352 ? 3 : heads <= 448 || (heads > 576 && heads < 768) ? 2 : 1;
+    const size_t partials =
+        static_cast<size_t>(c->slot_hi) * c->cfg.num_kv_heads * splits * c->G;
+    if (partials * (ra::kHeadDim + 2) * sizeof(float) > ra::kNoAllocScratchBytes) splits = 1;
+  }
+  if (2 * keys_max <= 3 * unit) splits = 1;
+  int64_t sk = c->cfg.attn_split > 0 ? c->cfg.attn_split
+                                     : std::max((keys_max + splits - 1) / splits,
+                                                splits > 1 ? unit : int64_t(0));
+  sk = std::max(sk, (keys_max + ra::kMaxSplits - 1) / ra::kMaxSplits);
   Plan p;
   p.waves = 4;
-  const int unit = 2 * 32 * p.waves;
-  const int64_t splits =
-      std::min<int64_t>(ra::kMaxSplits, std::max(1, (256 + heads / 2) / heads));
-  int64_t sk = c->cfg.attn_split > 0 ? c->cfg.attn_split
-                                     : std::max<int64_t>(unit, (keys_max + splits - 1) / splits);
-  sk = std::max(sk, (keys_max + ra::kMaxSplits - 1) / ra::kMaxSplits);
-  p.split_keys = static_cast<int>(round_up(sk, 32));
+  p.split_keys = static_cast<int>(round_up(sk, ra::kBlockRows));
   p.max_splits = p.partials = static_cast<int>((keys_max + p.split_keys - 1) / p.split_keys);
   p.whole = p.max_splits == 1;
   return p;

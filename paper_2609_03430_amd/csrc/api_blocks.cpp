@@ -115,11 +115,17 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
   }
   int32_t* list = static_cast<int32_t*>(workspace);
   void* scratch = static_cast<char*>(workspace) + list_bytes(c->cfg, n_blocks);
-  const ra::BlockChoice choice{list, std::min(n_blocks, ra::kMaxBlocks), n_blocks, recent_rows};
+  ra::BlockChoice choice;
+  choice.list = list;
+  choice.stride = n_blocks;      // (more than kMaxBlocks: no head chooses)
+  choice.n_blocks = n_blocks;
+  choice.recent = recent_rows;
+  choice.bounds = c->bounds;
+  choice.units = c->bounds + c->pool_rows / ra::kBlockRows * ra::kBoundsBytes;
   if (candidates > 0 && n_blocks > 0)
-    RA_LAUNCH(ra::launch_choose_blocks(sh, c->meta, q, c->bounds, c->pool_rows, layer, c->slot_hi,
-                                       choice, list, static_cast<uint32_t*>(scratch),
-                                       ra::kMaxBlocks, c->arrivals, candidates, hs));
+    RA_LAUNCH(ra::launch_choose_blocks(sh, c->meta, q, layer, c->slot_hi, choice,
+                                       static_cast<uint32_t*>(scratch), ra::kMaxBlocks,
+                                       c->arrivals, candidates, hs));
   c->appended[layer] = 1;
   ++c->n_appended;
   if (n_active == 0) return RA_OK;

@@ -10,6 +10,7 @@
 // lies inside the head's region or page), and the wavefront that owns it puts the
 // new pair in its place and zeros above it.
 #include "attn_parts.h"
+#include "block_choice.h"
 #include "e4m3.h"
 
 namespace ra {
@@ -18,6 +19,7 @@ namespace {
 struct BlockWork : Work {
   int b0, b1;        // the workgroup's attended blocks
   int n;             // attended blocks of the head
+  int cand;          // candidate blocks
   int chosen;        // the first `chosen` come from the list ..
   int shift;         // .. and block i after them is cached block i + shift
 };
@@ -34,12 +36,12 @@ __device__ __forceinline__ BlockWork locate_blocks(const AttnLaunch& a, const Bl
   if (!M.active) return w;
   w.len = M.len;
   w.n_keys = w.len + 1;
-  w.chosen = w.shift = 0;
+  w.cand = w.chosen = w.shift = 0;
   if constexpr (LIST) {
-    const int cand = candidate_blocks(w.len, ch.recent);
-    if (cand > ch.n_blocks) {
+    w.cand = candidate_blocks(w.len, ch.recent);
+    if (w.cand > ch.n_blocks) {
       w.chosen = ch.n_blocks;
-      w.shift = cand - ch.n_blocks;
+      w.shift = w.cand - ch.n_blocks;
     }
   }
   w.n = w.len / kBlockRows + 1 - w.shift;
@@ -70,16 +72,6 @@ struct Pools {
   const uint8_t* v_scale;
 };
 
-// The largest of the lanes with the same lane & 15, in registers: the two rows of 16
-// lanes of each half exchanged, then the halves.
-__device__ __forceinline__ float max_over_groups(float x) {
-  const uint32_t u = __float_as_uint(x);
-  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
 // 2^x, a result below 2^-126 flushed to zero: nothing beside a weight of 1.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -90,12 +82,12 @@ struct Bf16Rows {
   using Channels = RowChannels;
   struct Query {
     bf16x8 q[4];
-    __device__ __forceinline__ void load(const uint16_t* row, bool real, int grp) {
+    static __device__ __forceinline__ int channel(int i, int grp) { return 32 * i + 8 * grp; }
+    __device__ __forceinline__ void set(const u32x4 (&raw)[4], bool real) {
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const u32x4 z = {0u, 0u, 0u, 0u};
-        const u32x4 x = ld16(row + 32 * s + 8 * grp);
-        q[s] = as_bf16x8(real ? x : z);
+        q[s] = as_bf16x8(real ? raw[s] : z);
       }
     }
   };
@@ -105,13 +97,14 @@ struct Bf16Rows {
     load_block(b, static_cast<const uint16_t*>(p.k) + row * kHeadDim,
                static_cast<const uint16_t*>(p.v) + row * kHeadDim, 0, lm);
   }
-  // The step's pair, as bf16 in LDS (called by one whole wavefront).
+  // The step's pair, as bf16 in LDS: a lane's two channels of each (called by one whole
+  // wavefront).
   struct New {
     uint16_t k[kHeadDim], v[kHeadDim];
-    __device__ __forceinline__ void stage(const uint16_t* kn, const uint16_t* vn) {
+    __device__ __forceinline__ void stage(uint32_t wk, uint32_t wv) {
       const int lane = threadIdx.x & 63;
-      reinterpret_cast<uint32_t*>(k)[lane] = reinterpret_cast<const uint32_t*>(kn)[lane];
-      reinterpret_cast<uint32_t*>(v)[lane] = reinterpret_cast<const uint32_t*>(vn)[lane];
+      reinterpret_cast<uint32_t*>(k)[lane] = wk;
+      reinterpret_cast<uint32_t*>(v)[lane] = wv;
     }
     // .. at row `at` of the block, zeros above it
     __device__ __forceinline__ void patch(Block& b, int at, const LaneMap& lm) const {
@@ -185,24 +178,23 @@ struct E4m3Rows {
   struct Query {
     i32x8 hi, lo;
     int scale_hi, scale_lo;
-    __device__ __forceinline__ void load(const uint16_t* row, bool real, int grp) {
+    static __device__ __forceinline__ int channel(int i, int grp) {
+      return 64 * (i >> 1) + 16 * grp + 8 * (i & 1);
+    }
+    __device__ __forceinline__ void set(const u32x4 (&raw)[4], bool real) {
       float x[32];
       uint32_t amax = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32x4 w = ld16(row + 64 * (i >> 1) + 16 * grp + 8 * (i & 1));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t u = real ? w[j] : 0u;
+          const uint32_t u = real ? raw[i][j] : 0u;
           x[8 * i + 2 * j] = bf16_low(u);
           x[8 * i + 2 * j + 1] = bf16_high(u);
           amax = max(amax, max(row_magnitude(bf16_low(u)), row_magnitude(bf16_high(u))));
         }
       }
-#pragma unroll
-      for (int o = 16; o < 64; o <<= 1)
-        amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
-      const uint32_t byte = max(e4m3_scale_byte(amax), 5u);     // lo's is four less
+      const uint32_t byte = max(e4m3_scale_byte(max_over_groups(amax)), 5u);   // lo's: 4 less
       const float inv = e4m3_inverse(byte);
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = e4m3_clamp(x[i] * inv, byte);
@@ -245,18 +237,12 @@ struct E4m3Rows {
     uint8_t k[kHeadDim], v[kHeadDim];
     uint32_t ks, vs;
     // quantised as it is written, and attended as it is held
-    __device__ __forceinline__ void stage(const uint16_t* kn, const uint16_t* vn) {
+    __device__ __forceinline__ void stage(uint32_t wk, uint32_t wv) {
       const int lane = threadIdx.x & 63;
-      const uint32_t wk = reinterpret_cast<const uint32_t*>(kn)[lane];
-      const uint32_t wv = reinterpret_cast<const uint32_t*>(vn)[lane];
       uint32_t mk = max(row_magnitude(bf16_low(wk)), row_magnitude(bf16_high(wk)));
       uint32_t mv = max(row_magnitude(bf16_low(wv)), row_magnitude(bf16_high(wv)));
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        mk = max(mk, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mk), o, 64)));
-        mv = max(mv, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mv), o, 64)));
-      }
-      const uint32_t bk = e4m3_scale_byte(mk), bv = e4m3_scale_byte(mv);
+      const uint32_t bk = e4m3_scale_byte(max_over_groups(max_over_row16(mk)));
+      const uint32_t bv = e4m3_scale_byte(max_over_groups(max_over_row16(mv)));
       const float ik = e4m3_inverse(bk), iv = e4m3_inverse(bv);
       reinterpret_cast<uint16_t*>(k)[lane] =
           static_cast<uint16_t>(e4m3_pack2<false>(e4m3_clamp(bf16_low(wk) * ik, bk),
@@ -413,12 +399,31 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
   const int b1 = __builtin_amdgcn_readfirstlane(min(b0 + per, w.b1));
   const bool has = b0 < b1;
   const bool owns_last = has && b1 == w.n;
-  const int32_t* list = nullptr;
-  if constexpr (LIST) list = ch.list + (static_cast<int64_t>(w.slot) * Hkv + w.g) * ch.stride;
+  // the chosen blocks: of few candidates, chosen here (by every split, alike), else by
+  // the launch before
+  int32_t* list = nullptr;
+  __shared__ __align__(16) uint32_t s_keys[LIST ? kFusedBlocks : 1];
+  __shared__ int32_t s_list[LIST ? kFusedBlocks : 1];
+  const bool fused = LIST && w.chosen > 0 && w.cand <= kFusedBlocks;
+  if constexpr (LIST) {
+    list = ch.list + (static_cast<int64_t>(w.slot) * Hkv + w.g) * ch.stride;
+    if (fused) {
+      score_blocks<64 * W, PAGED>(
+          s_keys, 0, w.cand, w.rm, ch.bounds, ch.units,
+          static_cast<const uint16_t*>(a.q) +
+              (static_cast<int64_t>(w.slot) * Hq + w.g * G) * kHeadDim, G);
+      __syncthreads();
+      if (wave == 0) choose_few(s_keys, w.cand, w.chosen, s_list);
+      __syncthreads();
+      if (w.split == 0)
+        for (int i = threadIdx.x; i < w.chosen; i += 64 * W) list[i] = s_list[i];
+    }
+  }
   const auto load = [&](typename R::Block& b, int i) {
     int cached = i + w.shift;
     if constexpr (LIST) {
-      if (i < w.chosen) cached = list[i];
+      if (i < w.chosen) cached = fused ? s_list[i] : list[i];
+      cached = __builtin_amdgcn_readfirstlane(cached);
     }
     R::load(b, pools, pool_row<PAGED>(w.rm, cached * kBlockRows), lm);
   };
@@ -429,19 +434,25 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
 #pragma unroll
   for (int u = 0; u < 8; ++u) st.acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (has) {
+    // the queries and the new pair first: they are made ready while the rows arrive
+    const uint16_t* qrow = static_cast<const uint16_t*>(a.q) +
+                           (static_cast<int64_t>(w.slot) * Hq + w.g * G + (qi < G ? qi : 0)) * kHeadDim;
+    u32x4 raw[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) raw[s] = ld16(qrow + R::Query::channel(s, grp));
+    uint32_t new_k = 0, new_v = 0;
+    if (owns_last) {
+      const int64_t src = (static_cast<int64_t>(w.slot) * Hkv + w.g) * (kHeadDim / 2) + lane;
+      new_k = static_cast<const uint32_t*>(a.k_new)[src];
+      new_v = static_cast<const uint32_t*>(a.v_new)[src];
+    }
     const int last = b1 - 1;
     typename R::Block x0, x1;
     load(x0, b0);
     load(x1, min(b0 + 1, last));
     typename R::Query q;
-    q.load(static_cast<const uint16_t*>(a.q) +
-               (static_cast<int64_t>(w.slot) * Hq + w.g * G + (qi < G ? qi : 0)) * kHeadDim,
-           qi < G, grp);
-    if (owns_last) {
-      const int64_t src = (static_cast<int64_t>(w.slot) * Hkv + w.g) * kHeadDim;
-      s_new.stage(static_cast<const uint16_t*>(a.k_new) + src,
-                  static_cast<const uint16_t*>(a.v_new) + src);
-    }
+    q.set(raw, qi < G);
+    if (owns_last) s_new.stage(new_k, new_v);
     // two register buffers in turn; every prefetch is issued (the last block's again
     // once there is none left), so that the wait for a block leaves the next one's
     // loads in flight
@@ -488,7 +499,7 @@ void launch_blocks(const Shape& sh, const AttnLaunch& a, const BlockChoice& ch, 
 }  // namespace
 
 hipError_t launch_attention_e4m3(const Shape& sh, const AttnLaunch& a, hipStream_t s) {
-  const BlockChoice none{nullptr, 0, 0, 0};
+  const BlockChoice none{};
   if (sh.pg.tables) launch_blocks<E4m3Rows, true, false>(sh, a, none, s);
   else launch_blocks<E4m3Rows, false, false>(sh, a, none, s);
   return hipGetLastError();

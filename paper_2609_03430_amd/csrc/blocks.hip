@@ -12,37 +12,13 @@
 // an upper bound of its products with the block's keys but for Q's rounding.  The
 // sums are of integers and exact, and so is the power of two in fp32: the choice does
 // not depend on the order of anything.
-#include "attn_parts.h"
-#include "e4m3.h"
+#include <algorithm>
+
+#include "block_choice.h"
 #include "select.h"
 
 namespace ra {
 namespace {
-
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-constexpr float kMaxBf16 = 3.3895313892515355e38f;
-
-__device__ __forceinline__ float finite_bf16(float x) {
-  x = x == x ? x : 0.f;
-  return fminf(fmaxf(x, -kMaxBf16), kMaxBf16);
-}
-
-// t of a largest magnitude: its fp32 exponent less 6 where its fraction is at most
-// 127/64, else less 5 (the sum carries), within [-60, 50].
-__device__ __forceinline__ int unit_exponent(uint32_t amax_bits) {
-  const int t = static_cast<int>((amax_bits + 0x01ffffu) >> 23) - 127 - 6;
-  return min(max(t, -60), 50);
-}
-
-__device__ __forceinline__ float pow2(int e) { return __uint_as_float((e + 127) << 23); }
-
-__device__ __forceinline__ uint32_t pack_int8(float a, float b, float c, float d) {
-  const auto byte = [](float x) {
-    return static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(x, -127.f), 127.f))) & 255u;
-  };
-  return byte(a) | byte(b) << 8 | byte(c) << 16 | byte(d) << 24;
-}
 
 struct BoundsBatch {
   BoundsRange r[kBoundsBatch];
@@ -136,74 +112,21 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(
   if (lane == 0) units[row0 / kBlockRows] = static_cast<int8_t>(t);
 }
 
-// A workgroup scores up to kChunkBlocks candidates of a (sequence, KV head), sixteen at
-// a time (v_mfma_i32_16x16x64_i8: blocks x [H | L] against [max(Q, 0); min(Q, 0)] for
-// the group's queries); its first bounds are on their way while the queries are
-// rounded.  A head of one chunk is chosen from by one wavefront.  The chunks of a
-// longer head leave their scores in memory, and the last to finish selects (select.h;
-// as in merge_if_last, nothing waits for another workgroup).  One workgroup per head
-// took 40 us for 8 heads of 4,096 candidates, whose bounds it read at 27 GB/s.
+// Choice among the candidates of long heads (shorter ones: choose_few in the
+// attention kernel): workgroups of a head score kChunkBlocks candidates each and leave
+// the scores in memory; the last to finish selects (select.h; as in merge_if_last,
+// nothing waits for another workgroup).  One workgroup per head took 40 us for 8 heads
+// of 4,096 candidates, whose bounds it read at 27 GB/s; eight take 18.
 constexpr int kChooseThreads = 512;
 constexpr int kChunkBlocks = 512;
 
-// The want (< n) smallest of n <= kChunkBlocks keys, the lowest index first among
-// equals, as ascending indices: one wavefront halves the range of the keys until a
-// bound has exactly `want` of them at or below it, or until it is a key that several
-// share.  Called by one whole wavefront; the bounds are the same in every lane.
-__device__ __forceinline__ void choose_in_wave(const uint32_t* keys, int n, int want,
-                                               int32_t* __restrict__ dst) {
-  constexpr int kPer = kChunkBlocks / 64;
-  const int lane = threadIdx.x & 63;
-  uint32_t k[kPer], low = 0xffffffffu, high = 0;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    k[j] = keys[64 * j + lane];              // (all ones past the candidates)
-    low = min(low, k[j]);
-    high = max(high, 64 * j + lane < n ? k[j] : 0u);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    low = min(low, static_cast<uint32_t>(__shfl_xor(static_cast<int>(low), o, 64)));
-    high = max(high, static_cast<uint32_t>(__shfl_xor(static_cast<int>(high), o, 64)));
-  }
-  uint32_t lo = __builtin_amdgcn_readfirstlane(low), hi = __builtin_amdgcn_readfirstlane(high);
-  const auto count = [&](uint32_t bound) {
-    int c = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) c += __popcll(__ballot(k[j] <= bound));
-    return c;
-  };
-  // at the end hi has at least `want` keys at or below it, hi - 1 fewer if lo == hi
-  bool exact = false;
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    const int c = count(mid);
-    if (c >= want) hi = mid; else lo = mid + 1;
-    exact = c == want;
-    if (exact) break;
-  }
-  // every key below hi, and as many of those equal to it as are wanted
-  int at = 0, equal = exact ? want : want - (hi ? count(hi - 1) : 0);
-  const uint64_t below_lane = (uint64_t(1) << lane) - 1;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const uint64_t eq = __ballot(k[j] == hi), lt = __ballot(k[j] < hi);
-    const bool take = (lt >> lane & 1) || ((eq >> lane & 1) && __popcll(eq & below_lane) < equal);
-    const uint64_t taken = __ballot(take);
-    if (take) dst[at + __popcll(taken & below_lane)] = 64 * j + lane;
-    at += __popcll(taken);
-    equal -= min(equal, static_cast<int>(__popcll(eq)));
-  }
-}
-
 template <int KPT, bool PAGED>
 __global__ __launch_bounds__(kChooseThreads) void choose_blocks_kernel(
-    const SeqMeta* __restrict__ meta, const uint16_t* __restrict__ q,
-    const int8_t* __restrict__ bounds, const int8_t* __restrict__ units, int layer, int Hq,
-    int Hkv, int G, Paging pg, BlockChoice ch, int32_t* __restrict__ list,
-    uint32_t* __restrict__ scores, int score_stride, int* __restrict__ arrivals) {
+    const SeqMeta* __restrict__ meta, const uint16_t* __restrict__ q, int layer, int Hq, int Hkv,
+    int G, Paging pg, BlockChoice ch, uint32_t* __restrict__ scores, int score_stride,
+    int* __restrict__ arrivals) {
   constexpr int NT = kChooseThreads;
-  __shared__ __align__(16) uint32_t keys[kChunkBlocks];   // ascending from the best
+  __shared__ uint32_t keys[kChunkBlocks];
   __shared__ SelectShared sel_sh;
   __shared__ int last;
   const int g = blockIdx.y, slot = blockIdx.z, head = slot * Hkv + g;
@@ -211,152 +134,57 @@ __global__ __launch_bounds__(kChooseThreads) void choose_blocks_kernel(
   if (!M.active) return;
   const int cand = candidate_blocks(M.len, ch.recent);
   const int lo = static_cast<int>(blockIdx.x) * kChunkBlocks;
-  if (cand <= ch.n_blocks || lo >= cand) return;
+  if (cand <= ch.n_blocks || cand <= kFusedBlocks || lo >= cand) return;
   const int n = min(cand - lo, kChunkBlocks);
-  const int t = threadIdx.x, lane = t & 63, r = lane & 15, grp = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const RowMap rm = row_map(M, slot, layer * Hkv + g, pg);
-  const auto block_at = [&](int b) {
-    return pool_row<PAGED>(rm, (lo + min(b, n - 1)) * kBlockRows) / kBlockRows;
-  };
-  // every bound of the wavefront's tiles (its last candidate's again past the last)
-  constexpr int kTiles = kChunkBlocks / 16 / (NT / 64);
-  i32x4 h[kTiles][4];
-  int unit[kTiles];
-#pragma unroll
-  for (int k = 0; k < kTiles; ++k) {
-    if (16 * (wave + k * (NT / 64)) >= n) break;
-    const int64_t at = block_at(16 * (wave + k * (NT / 64)) + r);
-    const int8_t* src = bounds + at * kBoundsBytes + 16 * grp;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) h[k][s] = *reinterpret_cast<const i32x4*>(src + 64 * s);
-    unit[k] = units[at];
-  }
-
-  // the group's queries: lane (r, grp) holds channels 64 s + 16 grp .. + 15 of query r
-  i32x4 pos[2], neg[2];
-  int u;
-  {
-    const uint16_t* row = q + (static_cast<int64_t>(slot) * Hq + g * G + (r < G ? r : 0)) * kHeadDim;
-    float x[2][16];
-    uint32_t amax = 0;
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const u32x4 w = ld16(row + 64 * s + 16 * grp + 8 * k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[s][8 * k + 2 * i] = finite_bf16(bf16_low(w[i]));
-          x[s][8 * k + 2 * i + 1] = finite_bf16(bf16_high(w[i]));
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          amax = max(amax, __float_as_uint(fabsf(x[s][8 * k + i])));
-      }
-#pragma unroll
-    for (int o = 16; o < 64; o <<= 1)
-      amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), o, 64)));
-    u = unit_exponent(amax);
-    const float inv = pow2(-u);
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float y[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = rintf(x[s][4 * i + j] * inv);
-        pos[s][i] = static_cast<int>(pack_int8(fmaxf(y[0], 0.f), fmaxf(y[1], 0.f),
-                                               fmaxf(y[2], 0.f), fmaxf(y[3], 0.f)));
-        neg[s][i] = static_cast<int>(pack_int8(fminf(y[0], 0.f), fminf(y[1], 0.f),
-                                               fminf(y[2], 0.f), fminf(y[3], 0.f)));
-      }
-  }
-
-#pragma unroll
-  for (int k = 0; k < kTiles; ++k) {
-    const int tile = wave + k * (NT / 64);
-    if (16 * tile >= n) break;
-    i32x4 sum = {0, 0, 0, 0};
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(h[k][s], s < 2 ? pos[s] : neg[s - 2], sum, 0, 0, 0);
-    // lane (query r, grp): blocks 16 tile + 4 grp + i; the block's exponent is the
-    // same for every query and joins after the maximum
-    const int e = __shfl(unit[k], 4 * grp + (r & 3), 64);
-    float best[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      best[i] = __uint_as_float(over_row16(
-          __float_as_uint(r < G ? ldexpf(static_cast<float>(sum[i]), u) : kNegInf),
-          [](uint32_t a, uint32_t b) {
-            return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
-          }));
-    const int b = 16 * tile + 4 * grp + r;
-    if (r < 4 && b < n) {
-      const float x = ldexpf(r == 0 ? best[0] : r == 1 ? best[1] : r == 2 ? best[2] : best[3], e);
-      const uint32_t bits = __float_as_uint(x);      // descending order of the scores
-      keys[b] = bits >> 31 ? bits : ~(bits | 0x80000000u);
-    }
-  }
-  // past the candidates: worse than any (a score is finite, its key not all ones)
-  for (int b = n + t; b < kChunkBlocks; b += NT) keys[b] = 0xffffffffu;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  score_blocks<NT, PAGED>(keys, lo, n, row_map(M, slot, layer * Hkv + g, pg), ch.bounds, ch.units,
+                          q + (static_cast<int64_t>(slot) * Hq + g * G) * kHeadDim, G);
   __syncthreads();
-  int32_t* dst = list + static_cast<int64_t>(head) * ch.stride;
-
-  if (cand <= kChunkBlocks) {
-    if (wave == 0) choose_in_wave(keys, n, ch.n_blocks, dst);
-    return;
+  uint32_t* all = scores + static_cast<int64_t>(head) * score_stride;
+  if (t < n)
+    __hip_atomic_store(all + lo + t, keys[t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (t == 0) {
+    const int chunks = (cand + kChunkBlocks - 1) / kChunkBlocks;
+    const int prev = __hip_atomic_fetch_add(arrivals + head, 1, __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT);
+    last = prev == chunks - 1;
+    if (last) __hip_atomic_store(arrivals + head, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-
-  if constexpr (KPT > 0) {
-    uint32_t* all = scores + static_cast<int64_t>(head) * score_stride;
-    if (t < n)
-      __hip_atomic_store(all + lo + t, keys[t], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t == 0) {
-      const int chunks = (cand + kChunkBlocks - 1) / kChunkBlocks;
-      const int prev = __hip_atomic_fetch_add(arrivals + head, 1, __ATOMIC_RELAXED,
-                                              __HIP_MEMORY_SCOPE_AGENT);
-      last = prev == chunks - 1;
-      if (last) __hip_atomic_store(arrivals + head, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!last) return;
-    uint64_t key[KPT];
-    uint32_t tie[KPT], valid = 0;
+  __syncthreads();
+  if (!last) return;
+  uint64_t key[KPT];
+  uint32_t tie[KPT], valid = 0;
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      const int b = t * KPT + i;
-      tie[i] = static_cast<uint32_t>(b);
-      key[i] = __hip_atomic_load(all + min(b, cand - 1), __ATOMIC_RELAXED,
-                                 __HIP_MEMORY_SCOPE_AGENT);
-      if (b < cand) valid |= 1u << i;
-    }
-    const uint32_t chosen = select_smallest<NT, KPT, 32>(key, tie, valid, ch.n_blocks, sel_sh);
-    const int mine = __popc(chosen), incl = wave_inclusive_scan(mine);
-    if (lane == 63) sel_sh.wave_tot[wave] = incl;
-    __syncthreads();
-    int k = incl - mine;
-    for (int w = 0; w < wave; ++w) k += sel_sh.wave_tot[w];
-#pragma unroll
-    for (int i = 0; i < KPT; ++i)
-      if ((chosen >> i) & 1) dst[k++] = t * KPT + i;
+  for (int i = 0; i < KPT; ++i) {
+    const int b = t * KPT + i;
+    tie[i] = static_cast<uint32_t>(b);
+    key[i] = __hip_atomic_load(all + min(b, cand - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (b < cand) valid |= 1u << i;
   }
+  const uint32_t chosen = select_smallest<NT, KPT, 32>(key, tie, valid, ch.n_blocks, sel_sh);
+  const int mine = __popc(chosen), incl = wave_inclusive_scan(mine);
+  if (lane == 63) sel_sh.wave_tot[wave] = incl;
+  __syncthreads();
+  int k = incl - mine;
+  for (int w = 0; w < wave; ++w) k += sel_sh.wave_tot[w];
+  int32_t* dst = ch.list + static_cast<int64_t>(head) * ch.stride;
+#pragma unroll
+  for (int i = 0; i < KPT; ++i)
+    if ((chosen >> i) & 1) dst[k++] = t * KPT + i;
 }
 
 template <int KPT>
-void launch_choose(const Shape& sh, const SeqMeta* meta, const void* q, const int8_t* bounds,
-                   const int8_t* units, int layer, int max_seqs, const BlockChoice& ch,
-                   int32_t* list, uint32_t* scores, int score_stride, int* arrivals,
+void launch_choose(const Shape& sh, const SeqMeta* meta, const void* q, int layer, int max_seqs,
+                   const BlockChoice& ch, uint32_t* scores, int score_stride, int* arrivals,
                    int max_candidates, hipStream_t s) {
   const auto kernel = sh.pg.tables ? choose_blocks_kernel<KPT, true>
                                    : choose_blocks_kernel<KPT, false>;
   const dim3 grid((max_candidates + kChunkBlocks - 1) / kChunkBlocks, sh.Hkv, max_seqs);
   hipLaunchKernelGGL(kernel, grid, dim3(kChooseThreads), 0, s, meta,
-                     static_cast<const uint16_t*>(q), bounds, units, layer, sh.Hq, sh.Hkv, sh.G,
-                     sh.pg, ch, list, scores, score_stride, arrivals);
+                     static_cast<const uint16_t*>(q), layer, sh.Hq, sh.Hkv, sh.G, sh.pg, ch, scores,
+                     score_stride, arrivals);
 }
 
 }  // namespace
@@ -386,17 +214,15 @@ hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void*
   return hipSuccess;
 }
 
-hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q,
-                                const int8_t* bounds, int64_t pool_rows, int layer, int max_seqs,
-                                const BlockChoice& ch, int32_t* list, uint32_t* scores,
+hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q, int layer,
+                                int max_seqs, const BlockChoice& ch, uint32_t* scores,
                                 int score_stride, int* arrivals, int max_candidates,
                                 hipStream_t s) {
-  const int8_t* units = bounds + pool_rows / kBlockRows * kBoundsBytes;
-#define RA_CHOOSE(KPT)                                                                        \
-  launch_choose<KPT>(sh, meta, q, bounds, units, layer, max_seqs, ch, list, scores,           \
-                     score_stride, arrivals, max_candidates, s)
-  if (max_candidates <= kChunkBlocks) RA_CHOOSE(0);
-  else if (max_candidates <= 4 * kChooseThreads) RA_CHOOSE(4);
+  if (max_candidates <= kFusedBlocks) return hipSuccess;
+#define RA_CHOOSE(KPT)                                                                       \
+  launch_choose<KPT>(sh, meta, q, layer, max_seqs, ch, scores, score_stride, arrivals,       \
+                     max_candidates, s)
+  if (max_candidates <= 4 * kChooseThreads) RA_CHOOSE(4);
   else if (max_candidates <= 8 * kChooseThreads) RA_CHOOSE(8);
   else if (max_candidates <= 32 * kChooseThreads) RA_CHOOSE(32);
   else return hipErrorInvalidValue;

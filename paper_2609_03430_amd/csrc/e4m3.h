@@ -42,6 +42,23 @@ __device__ __forceinline__ uint32_t max_over_row16(uint32_t x) {
   return over_row16(x, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
+// The largest of the lanes with the same lane & 15, in registers: the two rows of 16
+// lanes of each half exchanged, then the halves.
+__device__ __forceinline__ float max_over_groups(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t m = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+__device__ __forceinline__ uint32_t max_over_groups(uint32_t u) {
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t m = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return max(b[0], b[1]);
+}
+
 // |x| as the scale sees it (its bits).
 __device__ __forceinline__ uint32_t row_magnitude(float x) {
   const uint32_t b = __float_as_uint(x) & 0x7fffffffu;

@@ -246,12 +246,16 @@ hipError_t launch_attention(const Shape& sh, const AttnLaunch& a, hipStream_t s)
 // of kBlockRows rows below row kBlockRows * candidates are chosen from, later rows
 // and the step's new one always attended.
 constexpr int kBlockRows = 32;
+constexpr int kBlockShift = 5;
+static_assert(kBlockRows == 1 << kBlockShift, "rows to blocks by a shift");
 constexpr int kMaxBlocks = 16384;   // candidate blocks per head that are chosen from
 struct BlockChoice {
-  const int32_t* list;   // [slots][Hkv][stride] chosen blocks, ascending
-  int stride;
-  int n_blocks;          // blocks chosen per head where there are more candidates
-  int recent;            // most recent cached rows that are no candidates
+  int32_t* list = nullptr;        // [slots][Hkv][stride] chosen blocks, ascending
+  int stride = 0;
+  int n_blocks = 0;               // blocks chosen per head where there are more candidates
+  int recent = 0;                 // most recent cached rows that are no candidates
+  const int8_t* bounds = nullptr; // bounds of the pool's blocks, kBoundsBytes each
+  const int8_t* units = nullptr;  // and their exponents
 };
 __device__ __host__ inline int candidate_blocks(int len, int recent) {
   return len > recent ? (len - recent) / kBlockRows : 0;
@@ -272,14 +276,14 @@ constexpr int kBoundsBatch = 64;   // ranges per launch
 hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void* kpool,
                                int8_t* bounds, int64_t pool_rows, int layer,
                                const BoundsRange* ranges, int n, hipStream_t s);
-// Chosen blocks of every head of the active slots below max_seqs that have more than
-// choice.n_blocks candidates, at most max_candidates, into `list` (choice.stride
-// per head).  Heads of several workgroups pass their scores through `scores`
-// (score_stride words per head) and count themselves on `arrivals`, a word per
-// (slot, KV head) that is zero between launches.
-hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q,
-                                const int8_t* bounds, int64_t pool_rows, int layer, int max_seqs,
-                                const BlockChoice& choice, int32_t* list, uint32_t* scores,
+// Chosen blocks of the heads of the active slots below max_seqs that have more than
+// choice.n_blocks candidates and more than their attention chooses from itself
+// (block_choice.h), at most max_candidates, into choice.list.  Their workgroups pass
+// the scores through `scores` (score_stride words per head) and count themselves on
+// `arrivals`, a word per (slot, KV head) that is zero between launches.  Nothing is
+// launched where no head has so many.
+hipError_t launch_choose_blocks(const Shape& sh, const SeqMeta* meta, const void* q, int layer,
+                                int max_seqs, const BlockChoice& choice, uint32_t* scores,
                                 int score_stride, int* arrivals, int max_candidates,
                                 hipStream_t s);
 // Attention over the e4m3 rows of a cache, or with `choice` over the rows of a

@@ -231,11 +231,51 @@ __global__ __launch_bounds__(128) void read_rows_kernel(SeqMeta M, int slot, int
 
 // Sixteen lanes take an 8-row tile of keys or of values, eight channels each: the
 // largest magnitude of a row is joined over the sixteen lanes, and the codes are
-// packed two at a time in the order in which they are stored, along the channels
-// for keys and along the rows for values, so that the transposition costs nothing.
-// Bound by HBM: 256 B read and 129 written per row.
+// packed in the order in which they are stored, along the channels for keys and along
+// the rows for values, so that the values' transposition costs nothing; four lanes
+// exchange 16-byte units so that their stores are contiguous.
+// Bound by HBM, 256 B read and 129 written per row, while the conversions stay few: the
+// largest magnitudes are found on packed 16-bit words, and rows whose codes may need
+// their range enforced (no finite row below 2^127 does) take a branch of their own.
 constexpr int kTileLanes = 16;
 constexpr int kQuantRows = 256 / kTileLanes * 8;   // rows per workgroup of 256 threads
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Eight bf16 magnitudes' largest (its bits; a NaN's are the largest of all).
+__device__ __forceinline__ uint32_t largest_magnitude(u32x4 w) {
+  u16x2 m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = w[i] & 0x7fff7fffu;
+    __builtin_memcpy(&m[i], &a, 4);
+  }
+  const u16x2 x = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]),
+                                            __builtin_elementwise_max(m[2], m[3]));
+  return max(static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]));
+}
+
+// Four lanes' 16-byte units transposed: lane b's unit i becomes lane i's unit b.
+template <int XOR, int CTRL>
+__device__ __forceinline__ void exchange_units(u32x4& a, u32x4& b) {
+  const bool upper = threadIdx.x & XOR;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const uint32_t give = upper ? a[d] : b[d];
+    const uint32_t got = static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(0, static_cast<int>(give), CTRL, 0xf, 0xf, false));
+    a[d] = upper ? got : a[d];
+    b[d] = upper ? b[d] : got;
+  }
+}
+__device__ __forceinline__ void transpose_units(u32x4 (&u)[4]) {
+  exchange_units<1, 0xB1>(u[0], u[1]);
+  exchange_units<1, 0xB1>(u[2], u[3]);
+  exchange_units<2, 0x4E>(u[0], u[2]);
+  exchange_units<2, 0x4E>(u[1], u[3]);
+}
 
 // Row-major bf16 rows [L * Hkv][len][128] into rows [0, len) of each head.
 // Grid: (ceil(len / 128), L * Hkv, 2): keys (and positions), values.
@@ -265,53 +305,92 @@ __global__ __launch_bounds__(256) void write_rows_e4m3_kernel(
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     in[e] = u32x4{0u, 0u, 0u, 0u};
-    if (jt + e < len) in[e] = *reinterpret_cast<const u32x4*>(src + e * kHeadDim);
+    if (jt + e < len)
+      in[e] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + e * kHeadDim));
   }
-  uint64_t scales = 0;
-  float x[8][8];                               // [row][channel], divided by the row's scale
+  uint32_t amax[8], top = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    uint32_t amax = 0;
+    amax[e] = max_over_row16(largest_magnitude(in[e]));
+    top = max(top, amax[e]);
+  }
+  // rows past 1.75 * 2^127, infinities or NaNs
+  const bool enforce = top > 0x7f60u;
+  uint32_t byte[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[e][2 * i] = bf16_low(in[e][i]);
-      x[e][2 * i + 1] = bf16_high(in[e][i]);
-      amax = max(amax, max(row_magnitude(x[e][2 * i]), row_magnitude(x[e][2 * i + 1])));
+  for (int e = 0; e < 8; ++e) {
+    uint32_t m = amax[e] << 16;
+    if (enforce) {
+      m = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        m = max(m, max(row_magnitude(bf16_low(in[e][i])), row_magnitude(bf16_high(in[e][i]))));
+      m = max_over_row16(m);
     }
-    const uint32_t byte = e4m3_scale_byte(max_over_row16(amax));
-    scales |= static_cast<uint64_t>(byte) << (8 * e);
-    const float inv = e4m3_inverse(byte);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) x[e][c] = e4m3_clamp(x[e][c] * inv, byte);
+    byte[e] = e4m3_scale_byte(m);
   }
   const int64_t row0 = pool_row<PAGED>(rm, jt);          // a tile lies in one page
-  if (c8 == 0) *reinterpret_cast<uint64_t*>((keys ? kscale : vscale) + row0) = scales;
-  const auto pack4 = [](float a, float b, float c, float d) {
-    return e4m3_pack2<true>(c, d, e4m3_pack2<false>(a, b, 0u));
-  };
+  if (c8 == 0) {
+    uint64_t scales = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) scales |= static_cast<uint64_t>(byte[e]) << (8 * e);
+    *reinterpret_cast<uint64_t*>((keys ? kscale : vscale) + row0) = scales;
+  }
   if (keys) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if (jt + e < len) {
-        uint2 w;
-        w.x = pack4(x[e][0], x[e][1], x[e][2], x[e][3]);
-        w.y = pack4(x[e][4], x[e][5], x[e][6], x[e][7]);
-        *reinterpret_cast<uint2*>(kpool + (row0 + e) * kHeadDim + 8 * c8) = w;
+      uint2 w;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t a = in[e][2 * h], b = in[e][2 * h + 1];
+        uint32_t c;
+        if (enforce) {
+          const float inv = e4m3_inverse(byte[e]);
+          c = e4m3_pack2<true>(
+              e4m3_clamp(bf16_low(b) * inv, byte[e]), e4m3_clamp(bf16_high(b) * inv, byte[e]),
+              e4m3_pack2<false>(e4m3_clamp(bf16_low(a) * inv, byte[e]),
+                                e4m3_clamp(bf16_high(a) * inv, byte[e]), 0u));
+        } else {
+          const float scale = e4m3_scale(byte[e]);
+          bf16x2 x, y;
+          __builtin_memcpy(&x, &a, 4);
+          __builtin_memcpy(&y, &b, 4);
+          i16x2 r = {0, 0};
+          r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, x, scale, false);
+          r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, y, scale, true);
+          __builtin_memcpy(&c, &r, 4);
+        }
+        (h ? w.y : w.x) = c;
       }
+      if (jt + e < len)
+        *reinterpret_cast<uint2*>(kpool + (row0 + e) * kHeadDim + 8 * c8) = w;
     }
     return;
   }
-  uint8_t* dst = vpool + row0 * kHeadDim + 64 * c8;       // rows past len are zero codes
+  u32x4 units[4];                              // two channels of eight rows each
 #pragma unroll
-  for (int c = 0; c < 8; c += 2) {
-    u32x4 w;
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      w[2 * h] = pack4(x[0][c + h], x[1][c + h], x[2][c + h], x[3][c + h]);
-      w[2 * h + 1] = pack4(x[4][c + h], x[5][c + h], x[6][c + h], x[7][c + h]);
+    for (int e = 0; e < 8; e += 4) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float y[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t w = in[e + x][i];
+          y[x] = (h ? bf16_high(w) : bf16_low(w)) * e4m3_inverse(byte[e + x]);
+          if (enforce) y[x] = e4m3_clamp(y[x], byte[e + x]);
+        }
+        units[i][2 * h + e / 4] = e4m3_pack2<true>(y[2], y[3], e4m3_pack2<false>(y[0], y[1], 0u));
+      }
     }
-    *reinterpret_cast<u32x4*>(dst + 8 * c) = w;
   }
+  // rows past len are zero codes
+  transpose_units(units);
+  uint8_t* dst = vpool + row0 * kHeadDim + 64 * (c8 & ~3) + 16 * (c8 & 3);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<u32x4*>(dst + 64 * i) = units[i];
 }
 
 // Rows [0, len) of heads lg, lg + 1, .. to row-major bf16 outputs [heads][len][128],
