@@ -402,16 +402,31 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
   // the chosen blocks: of few candidates, chosen here (by every split, alike), else by
   // the launch before
   int32_t* list = nullptr;
-  __shared__ __align__(16) uint32_t s_keys[LIST ? kFusedBlocks : 1];
+  __shared__ uint32_t s_keys[LIST ? kFusedBlocks : 1];
   __shared__ int32_t s_list[LIST ? kFusedBlocks : 1];
+  __shared__ int32_t s_table[LIST && PAGED ? kFusedBlocks : 1];   // the candidates' pages
   const bool fused = LIST && w.chosen > 0 && w.cand <= kFusedBlocks;
+  // first pool row of a candidate block
+  const auto candidate_row = [&](int b) -> int64_t {
+    if constexpr (PAGED) {
+      const int shift = w.rm.page_shift - kBlockShift;
+      return s_table[b >> shift] * w.rm.group_rows + w.rm.head_off +
+             ((b & ((1 << shift) - 1)) << kBlockShift);
+    } else {
+      return w.rm.region + b * kBlockRows;
+    }
+  };
   if constexpr (LIST) {
     list = ch.list + (static_cast<int64_t>(w.slot) * Hkv + w.g) * ch.stride;
     if (fused) {
-      score_blocks<64 * W, PAGED>(
-          s_keys, 0, w.cand, w.rm, ch.bounds, ch.units,
-          static_cast<const uint16_t*>(a.q) +
-              (static_cast<int64_t>(w.slot) * Hq + w.g * G) * kHeadDim, G);
+      if constexpr (PAGED) {
+        const int pages = ((w.cand - 1) >> (w.rm.page_shift - kBlockShift)) + 1;
+        for (int i = threadIdx.x; i < pages; i += 64 * W) s_table[i] = w.rm.table[i];
+        __syncthreads();
+      }
+      score_blocks<64 * W>(s_keys, 0, w.cand, candidate_row, ch.bounds, ch.units,
+                           static_cast<const uint16_t*>(a.q) +
+                               (static_cast<int64_t>(w.slot) * Hq + w.g * G) * kHeadDim, G);
       __syncthreads();
       if (wave == 0) choose_few(s_keys, w.cand, w.chosen, s_list);
       __syncthreads();
@@ -420,12 +435,17 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
     }
   }
   const auto load = [&](typename R::Block& b, int i) {
-    int cached = i + w.shift;
-    if constexpr (LIST) {
-      if (i < w.chosen) cached = fused ? s_list[i] : list[i];
-      cached = __builtin_amdgcn_readfirstlane(cached);
+    int64_t row;
+    if (fused && i < w.chosen) {
+      row = candidate_row(__builtin_amdgcn_readfirstlane(s_list[i]));
+    } else {
+      int cached = i + w.shift;
+      if constexpr (LIST) {
+        if (i < w.chosen) cached = __builtin_amdgcn_readfirstlane(list[i]);
+      }
+      row = pool_row<PAGED>(w.rm, cached * kBlockRows);
     }
-    R::load(b, pools, pool_row<PAGED>(w.rm, cached * kBlockRows), lm);
+    R::load(b, pools, row, lm);
   };
 
   Softmax st;

@@ -78,15 +78,15 @@ template <int K, int STRIDE>
 struct ScoreTiles {
   i32x4 h[K][4];
   int unit[K];
-  template <bool PAGED>
-  __device__ __forceinline__ void load(int first, int lo, int n, const RowMap& rm,
+  template <typename RowOf>
+  __device__ __forceinline__ void load(int first, int lo, int n, const RowOf& row_of,
                                        const int8_t* bounds, const int8_t* units) {
     const int lane = threadIdx.x & 63, r = lane & 15, grp = lane >> 4;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if (16 * (first + k * STRIDE) >= n) break;
       const int b = lo + min(16 * (first + k * STRIDE) + r, n - 1);
-      const int64_t at = pool_row<PAGED>(rm, b * kBlockRows) >> kBlockShift;
+      const int64_t at = row_of(b) >> kBlockShift;
       const int8_t* src = bounds + at * kBoundsBytes + 16 * grp;
 #pragma unroll
       for (int s = 0; s < 4; ++s) h[k][s] = *reinterpret_cast<const i32x4*>(src + 64 * s);
@@ -127,9 +127,9 @@ struct ScoreTiles {
 // that ascend from the best: the wavefronts of the workgroup (NT threads, all of them
 // call) take sixteen blocks at a time (v_mfma_i32_16x16x64_i8: blocks x [H | L] against
 // [max(Q, 0); min(Q, 0)]); the first bounds are on their way while the queries are
-// rounded.
-template <int NT, bool PAGED>
-__device__ __forceinline__ void score_blocks(uint32_t* keys, int lo, int n, const RowMap& rm,
+// rounded.  row_of: the pool row at which a block of the head begins.
+template <int NT, typename RowOf>
+__device__ __forceinline__ void score_blocks(uint32_t* keys, int lo, int n, const RowOf& row_of,
                                              const int8_t* bounds, const int8_t* units,
                                              const uint16_t* queries, int G) {
   constexpr int kWaves = NT / 64;
@@ -140,14 +140,14 @@ __device__ __forceinline__ void score_blocks(uint32_t* keys, int lo, int n, cons
   for (int i = 0; i < 4; ++i)
     raw[i] = ld16(queries + (r < G ? r : 0) * kHeadDim + BlockQuery::channel(i, grp));
   ScoreTiles<4, kWaves> t;
-  t.template load<PAGED>(wave, lo, n, rm, bounds, units);
+  t.load(wave, lo, n, row_of, bounds, units);
   BlockQuery q;
   q.set(raw);
   for (int first = wave;;) {
     t.score(keys, first, n, q, G);
     first += 4 * kWaves;
     if (16 * first >= n) break;
-    t.template load<PAGED>(first, lo, n, rm, bounds, units);
+    t.load(first, lo, n, row_of, bounds, units);
   }
 }
 

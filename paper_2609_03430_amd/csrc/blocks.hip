@@ -116,9 +116,10 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(
 // attention kernel): workgroups of a head score kChunkBlocks candidates each and leave
 // the scores in memory; the last to finish selects (select.h; as in merge_if_last,
 // nothing waits for another workgroup).  One workgroup per head took 40 us for 8 heads
-// of 4,096 candidates, whose bounds it read at 27 GB/s; eight take 18.
+// of 4,096 candidates, whose bounds it read at 27 GB/s; with 512 candidates to a
+// workgroup a step took 38 to 40 us, with 256 36, with 128 37.
 constexpr int kChooseThreads = 512;
-constexpr int kChunkBlocks = 512;
+constexpr int kChunkBlocks = 256;
 
 template <int KPT, bool PAGED>
 __global__ __launch_bounds__(kChooseThreads) void choose_blocks_kernel(
@@ -137,8 +138,9 @@ __global__ __launch_bounds__(kChooseThreads) void choose_blocks_kernel(
   if (cand <= ch.n_blocks || cand <= kFusedBlocks || lo >= cand) return;
   const int n = min(cand - lo, kChunkBlocks);
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  score_blocks<NT, PAGED>(keys, lo, n, row_map(M, slot, layer * Hkv + g, pg), ch.bounds, ch.units,
-                          q + (static_cast<int64_t>(slot) * Hq + g * G) * kHeadDim, G);
+  const RowMap rm = row_map(M, slot, layer * Hkv + g, pg);
+  score_blocks<NT>(keys, lo, n, [&](int b) { return pool_row<PAGED>(rm, b * kBlockRows); },
+                   ch.bounds, ch.units, q + (static_cast<int64_t>(slot) * Hq + g * G) * kHeadDim, G);
   __syncthreads();
   uint32_t* all = scores + static_cast<int64_t>(head) * score_stride;
   if (t < n)
