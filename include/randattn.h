@@ -432,8 +432,8 @@ ra_status ra_evict_now(ra_cache* cache, int32_t seq, void* stream);
 size_t ra_sparse_bytes(const ra_config* cfg, int64_t pool_rows);
 
 /* Bytes of the workspace of a sparse step choosing n_blocks blocks per head (any
- * smaller n_blocks may use it too): the lists and the split partials.  0 as above or
- * if n_blocks < 0. */
+ * smaller n_blocks may use it too): the lists of chosen blocks, the scores and the
+ * split partials.  0 as above or if n_blocks < 0. */
 size_t ra_sparse_workspace_bytes(const ra_config* cfg, int32_t n_blocks);
 
 /* Attach a bounds buffer (ra_sparse_bytes bytes, 16-byte aligned; contents need not
@@ -445,7 +445,10 @@ ra_status ra_sparse_attach(ra_cache* cache, void* dev_bounds, size_t bounds_byte
 
 /* ra_decode_attention over the chosen blocks (see above): the same append, arrays,
  * step protocol and errors, one call per layer and step in its place (the layers of
- * a step may mix both).  RA_ERR_STATE if no bounds are attached or in graph mode;
+ * a step may mix both).  Afterwards the workspace begins with the lists, int32
+ * [max_seqs][Hkv][n_blocks], ascending, of the heads that had more candidates
+ * (others' are not set).  RA_ERR_STATE if no bounds are attached, in graph mode, or
+ * while `stream` is being captured (which bounds to compute is decided on the host);
  * RA_ERR_UNSUPPORTED for fp32, the hole-fill layout, or a head with more than 16384
  * candidates where that is more than n_blocks. */
 ra_status ra_sparse_attention(ra_cache* cache, int32_t layer, int32_t n_blocks,

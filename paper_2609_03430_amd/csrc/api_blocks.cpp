@@ -88,6 +88,11 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
   if (!workspace || workspace_bytes < ra_sparse_workspace_bytes(&c->cfg, n_blocks) ||
       (reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
     return RA_ERR_INVALID_ARG;
+  const hipStream_t hs = static_cast<hipStream_t>(stream);
+  // what to rebuild is decided here: a replay would not decide it again
+  hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+  RA_LAUNCH(hipStreamIsCapturing(hs, &capturing));
+  if (capturing != hipStreamCaptureStatusNone) return RA_ERR_STATE;
   // the attended rows of the longest step, and the blocks that need bounds first
   std::vector<ra::BoundsRange> ranges;
   int most = 0, n_active = 0, candidates = 0;
@@ -103,7 +108,6 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
     if (built < cand) ranges.push_back(ra::BoundsRange{s, built, cand});
   }
   if (candidates > ra::kMaxBlocks) return RA_ERR_UNSUPPORTED;
-  const hipStream_t hs = static_cast<hipStream_t>(stream);
   const ra_status grown = ra::host::grow_for_step(c, hs);
   if (grown != RA_OK) return grown;
   const ra::Shape sh = c->shape();

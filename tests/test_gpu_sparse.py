@@ -381,3 +381,144 @@ def test_refusals():
     assert status(B.ra_scored_evict, c.handle, 0, 1, B.make_scorer(0), w, w) \
         == B.RA_ERR_UNSUPPORTED
     c.close()
+
+
+def test_a_captured_step_is_refused():
+    """Nothing is launched into a capture, and the step goes on after it."""
+    run = _run(BF16, L=1, Hq=4, Hkv=2, K=100, lps=[150], r=8, every=8)
+    o = [oracle_of(run, 0)]
+    q, k, v = run.step_inputs(0)
+    out = torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        marker = torch.zeros(4, device=DEV)
+        st = status(run.cache.decode_sparse, 0, 2, 8, q, k, v, out)
+    assert st == B.RA_ERR_STATE
+    g.replay()
+    torch.cuda.synchronize()
+    assert marker.eq(0).all()
+    outs, _ = sparse_step(run, 2, 8)
+    check_step(run, o, outs, sparse=(2, 8, None))
+    run.close()
+
+
+@pytest.mark.parametrize("scorer", [B.RA_SCORER_SNAPKV, B.RA_SCORER_VASE])
+def test_after_a_scored_round(scorer):
+    """A score-based round drops prompt rows too: bounds from the first row on are
+    computed anew.  The rows are read back for the expected output."""
+    Hq, Hkv, n_blocks, recent = 8, 2, 3, 20
+    cfg = B.make_config(1, Hq, Hkv, 200, 16, 64, dtype=BF16, max_seqs=2,
+                        policy=B.RA_POLICY_EXTERNAL)
+    c = B.Cache(cfg, B.ra_required_slots(cfg, [150, 90]))
+    c.attach_sparse(n_blocks)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+
+    def rnd(*shape):
+        return torch.randn(*shape, 128, device=DEV, generator=gen).to(torch.bfloat16)
+    for i, lp in enumerate((150, 90)):
+        B.ra_seq_begin(c.handle, i, lp, 1, i, rnd(1, Hkv, lp), rnd(1, Hkv, lp))
+
+    def step(check):
+        q, k, v = rnd(2, Hq), rnd(2, Hkv), rnd(2, Hkv)
+        out = torch.empty_like(q)
+        before = [[torch.empty(B.ra_get_seq_info(c.handle, i).len, 128, dtype=torch.bfloat16,
+                               device=DEV) for _ in range(2 * Hkv)] for i in range(2)]
+        for i in range(2):
+            for h in range(Hkv):
+                B.ra_read_rows(c.handle, i, 0, h, before[i][2 * h], before[i][2 * h + 1])
+        c.decode_sparse(0, n_blocks, recent, q, k, v, out)
+        B.ra_end_step(c.handle)
+        if not check:
+            return
+        for i in range(2):
+            for h in range(Hkv):
+                K, V = (torch.cat([before[i][2 * h + j], x[i, h][None]]).double().cpu().numpy()
+                        for j, x in enumerate((k, v)))
+                mine = q[i, h * 4:h * 4 + 4].double().cpu().numpy()
+                rows = blocks.attended(mine, K, len(K) - 1, n_blocks, recent)
+                want = np.stack([softmax_attention(x, K[rows], V[rows]) for x in mine])
+                attn_err(out[i, h * 4:h * 4 + 4], want, B.RA_BF16, (i, h))
+    for round_ in range(2):
+        for t in range(205 if round_ == 0 else 40):
+            step(t % 40 == 0)
+        qwin = torch.randn(2, 1, Hq, 64, 128, device=DEV, generator=gen).to(torch.bfloat16)
+        scratch = torch.empty(B.ra_scored_scratch_bytes(cfg, 150), dtype=torch.uint8, device=DEV)
+        was = [B.ra_get_seq_info(c.handle, i).len for i in range(2)]
+        B.ra_scored_evict(c.handle, 0, 2, B.make_scorer(scorer), qwin, scratch)
+        assert all(B.ra_get_seq_info(c.handle, i).len <= was[i] for i in range(2))
+        for _ in range(3):
+            step(True)
+    assert all(B.ra_get_seq_info(c.handle, i).event >= 1 for i in range(2))
+    c.close()
+
+
+@pytest.mark.parametrize("layout", [CHRON, PAGED])
+def test_a_serving_run(layout):
+    """The operators together: an 8-bit cache whose first layer attends to every row
+    and whose second to part of them, requests admitted, preempted (their rows exported),
+    resumed in another slot and ended between steps."""
+    run = _run(E4M3, L=2, Hq=6, Hkv=2, K=120, lps=[100, 40, 70, 0], r=16, every=16, max_seqs=4,
+               layout=layout, page_rows=32, max_prompt_len=300, begin=False, pool_rows=6144)
+    rng = np.random.default_rng(11)
+    rep, saved, done, next_rid = {}, None, 0, 50
+
+    def admit(slot):
+        nonlocal next_rid
+        run.lps[slot], run.rids[slot] = int(rng.integers(0, 101)), next_rid
+        next_rid += 1
+        run.begin(slot)
+        rep[slot] = oracle_of(run, slot)
+    run.active = set()
+    for slot in (0, 1, 3):
+        admit(slot)
+    for t in range(220):
+        outs, _ = sparse_step(run, 2, 16, {1})
+        check_step(run, list(rep.values()), outs, (t,), (2, 16, {1}))
+        if t % 23 == 22 and saved is None:                      # preempt one
+            slot = int(rng.choice(sorted(rep)))
+            o = rep.pop(slot)
+            n = B.ra_get_seq_info(run.h, slot).len
+            kv = [torch.empty(2, 2, n, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+            B.ra_export_rows(run.h, slot, *kv)
+            run.end(slot)
+            saved = (o, run.steps[slot], run.lps[slot], run.rids[slot], run.seeds[slot], kv)
+        elif t % 23 == 10 and saved is not None:                # and resume it elsewhere
+            slot = int(rng.choice([s for s in range(4) if s not in rep]))
+            o, steps, lp, rid, seed, kv = saved
+            run.lps[slot], run.rids[slot], run.seeds[slot] = lp, rid, seed
+            B.ra_seq_begin(run.h, slot, lp, seed, rid)
+            B.ra_seq_fast_forward(run.h, slot, steps)
+            B.ra_write_rows(run.h, slot, *kv)
+            run.steps[slot] = steps
+            run.active.add(slot)
+            o.slot = slot
+            rep[slot], saved = o, None
+        elif t % 37 == 36:                                      # end one, admit another
+            slot = int(rng.choice(sorted(rep)))
+            rep.pop(slot)
+            run.end(slot)
+            admit(slot)
+            done += 1
+    check_heads(run, list(rep.values()))
+    assert done >= 3
+    run.close()
+
+
+def test_random_configurations():
+    rng = np.random.default_rng(78)
+    for trial in range(10):
+        Hkv, n = int(rng.integers(1, 4)), int(rng.integers(1, 4))
+        Hq = Hkv * int(rng.integers(1, 17))
+        lens = [int(x) for x in np.exp(rng.uniform(0, np.log(6000), n))]
+        layout, page_rows = int(rng.choice([CHRON, PAGED])), int(rng.choice([32, 64, 512]))
+        dtype, n_blocks, recent = int(rng.choice([BF16, E4M3])), int(rng.integers(0, 40)), int(
+            rng.integers(0, 200))
+        log("sparse trial %d: %s" % (trial, (Hq, Hkv, lens, layout, page_rows, dtype, n_blocks,
+                                             recent)))
+        keys, values, q, kn, vn = _inputs(trial, lens, Hq, Hkv, scale=0.5)
+        f = Fixed(dtype, Hq, Hkv, keys, values, layout, page_rows)
+        f.check(n_blocks, recent, q, kn, vn, (trial,))
+        f.check(n_blocks, recent, q, kn, vn, (trial, "again"))
+        f.close()
