@@ -467,6 +467,8 @@ ra_status launch_decode(ra_cache* c, int32_t layer, const void* q, const void* k
                         float* ws_ml, int split_stride, hipStream_t stream) {
   const ra_status grown = grow_for_step(c, stream);
   if (grown != RA_OK) return grown;
+  ra::Shape sh = c->shape();
+  if (c->cfg.dtype == RA_E4M3) sh.order = c->refresh_order();
   // rows of deferred events move in this step's attention where the plan
   // allows one workgroup per head; otherwise they move first, on their own
   bool move = false;
@@ -508,7 +510,7 @@ ra_status launch_decode(ra_cache* c, int32_t layer, const void* q, const void* k
     a.drops = c->drops;
     a.drop_stride = c->cfg.evict_every;
   }
-  const hipError_t e = ra::launch_attention(c->shape(), a, stream);
+  const hipError_t e = ra::launch_attention(sh, a, stream);
   if (e != hipSuccess) {
     c->appended[layer] = 0;
     --c->n_appended;

@@ -110,7 +110,8 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
   if (candidates > ra::kMaxBlocks) return RA_ERR_UNSUPPORTED;
   const ra_status grown = ra::host::grow_for_step(c, hs);
   if (grown != RA_OK) return grown;
-  const ra::Shape sh = c->shape();
+  ra::Shape sh = c->shape();
+  sh.order = c->refresh_order();
   if (!ranges.empty()) {
     RA_LAUNCH(ra::launch_block_bounds(sh, c->meta, c->kpool, c->bounds, c->pool_rows, layer,
                                       ranges.data(), static_cast<int>(ranges.size()), hs));

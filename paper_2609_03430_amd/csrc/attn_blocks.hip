@@ -26,11 +26,12 @@ struct BlockWork : Work {
 
 template <bool LIST>
 __device__ __forceinline__ BlockWork locate_blocks(const AttnLaunch& a, const BlockChoice& ch,
-                                                   int Hkv, const Paging& pg) {
+                                                   const SlotOrder& order, int Hkv,
+                                                   const Paging& pg) {
   BlockWork w;
   w.split = blockIdx.x;
   w.g = blockIdx.y;
-  w.slot = blockIdx.z;
+  w.slot = order.n ? order.slot[blockIdx.z] : blockIdx.z;
   const SeqMeta& M = a.meta[w.slot];
   w.valid = false;
   if (!M.active) return w;
@@ -57,7 +58,8 @@ __device__ __forceinline__ BlockWork locate_blocks(const AttnLaunch& a, const Bl
 
 // Splits of a head, for the merge.
 struct BlockSplits {
-  int recent, n_blocks;
+  int recent, n_blocks, at;
+  __device__ __forceinline__ int slot() const { return at; }
   __device__ __forceinline__ int operator()(const AttnLaunch& a, int slot) const {
     const int per = a.split_keys / kBlockRows;
     return (attended_blocks(a.meta[slot].len, recent, n_blocks) + per - 1) / per;
@@ -382,13 +384,13 @@ struct E4m3Rows {
 
 template <typename R, int W, int MINW, bool PAGED, bool LIST>
 __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
-    AttnLaunch a, BlockChoice ch, Paging pg, uint8_t* k_scale, uint8_t* v_scale, int G, int Hq,
-    int Hkv, float scale_log2) {
+    AttnLaunch a, BlockChoice ch, SlotOrder order, Paging pg, uint8_t* k_scale, uint8_t* v_scale,
+    int G, int Hq, int Hkv, float scale_log2) {
   __shared__ float s_m[W][kMaxGroup];
   __shared__ float s_l[W][kMaxGroup];
   __shared__ float s_o[W][kMaxGroup][kHeadDim];
   __shared__ __align__(16) typename R::New s_new;
-  const BlockWork w = locate_blocks<LIST>(a, ch, Hkv, pg);
+  const BlockWork w = locate_blocks<LIST>(a, ch, order, Hkv, pg);
   if (!w.valid) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, qi = lane & 15, grp = lane >> 4;
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
   if constexpr (!std::is_same_v<R, Bf16Rows>) R::gather_channels(st);
   finish_item<uint16_t, W, true, BlockSplits, typename R::Channels>(
       a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o,
-      LIST ? BlockSplits{ch.recent, ch.n_blocks} : BlockSplits{0, 1 << 30});
+      LIST ? BlockSplits{ch.recent, ch.n_blocks, w.slot} : BlockSplits{0, 1 << 30, w.slot});
   if (owns_last) {
     const int64_t row = pool_row<PAGED>(w.rm, w.len);
     s_new.append(a, row, k_scale, v_scale);
@@ -510,10 +512,11 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
 
 template <typename R, bool PAGED, bool LIST>
 void launch_blocks(const Shape& sh, const AttnLaunch& a, const BlockChoice& ch, hipStream_t s) {
-  const dim3 grid(a.max_splits, sh.Hkv, a.max_seqs);
+  const SlotOrder order = sh.order ? *sh.order : SlotOrder{};
+  const dim3 grid(a.max_splits, sh.Hkv, order.n ? order.n : a.max_seqs);
   const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(kHeadDim));
-  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, 2, PAGED, LIST>), grid, dim3(256), 0, s,
-                     a, ch, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
+  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, 2, PAGED, LIST>), grid, dim3(256), 0, s, a, ch,
+                     order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
 }
 
 }  // namespace

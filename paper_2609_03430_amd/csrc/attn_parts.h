@@ -110,6 +110,7 @@ struct Partial {
 
 // Splits of a head whose every cached row is attended.
 struct DenseSplits {
+  __device__ __forceinline__ int slot() const { return blockIdx.z; }
   __device__ __forceinline__ int operator()(const AttnLaunch& a, int slot) const {
     return (a.meta[slot].len + 1 + a.split_keys - 1) / a.split_keys;
   }
@@ -139,7 +140,7 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
                               const Splits& splits = Splits()) {
   __shared__ Partial s_part[NT];
   __shared__ int last;
-  const int slot = blockIdx.z, g = blockIdx.y, head = slot * Hkv + g;
+  const int slot = splits.slot(), g = blockIdx.y, head = slot * Hkv + g;
   const int nsplit = splits(a, slot);
   // This thread's partial stores are written before the workgroup counts
   // itself: the wait is issued as an asm statement that clobbers memory, so

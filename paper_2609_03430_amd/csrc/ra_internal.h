@@ -72,6 +72,14 @@ struct DueList {
   int slot[kDueList] = {};
 };
 
+// Slots in the order in which an attention launch takes them, the longest first (n =
+// 0: every slot, as they come).
+constexpr int kOrderMax = 256;
+struct SlotOrder {
+  int n = 0;
+  uint16_t slot[kOrderMax] = {};
+};
+
 struct Shape {
   int L, Hq, Hkv, G, r, every, dtype;  // dtype: 0 f32, 1 bf16, 2 e4m3 (bf16 in and out)
   int layout;                          // 0 chronological, 1 hole-fill, 2 paged
@@ -88,6 +96,7 @@ struct Shape {
   // e4m3 pools: the rows' scale bytes (e4m3.h)
   uint8_t* k_scale = nullptr;
   uint8_t* v_scale = nullptr;
+  const SlotOrder* order = nullptr;    // attention over blocks: the slots' order, if ragged
 };
 
 // Pool row of row j of one (sequence, layer, KV head) cache.
