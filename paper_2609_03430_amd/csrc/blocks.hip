@@ -21,18 +21,21 @@ namespace ra {
 namespace {
 
 struct BoundsBatch {
+  int n;                      // ranges
   BoundsRange r[kBoundsBatch];
+  int layer[kBoundsBatch];
 };
 
 // One wavefront per block: lane (c8, rows) reads eight channels of eight rows, the
 // four row groups join by shuffles.  Bound by HBM: the key rows, once per row that an
-// event or a write has changed.  Grid: (ceil(blocks / 4), Hkv, ranges).
+// event or a write has changed.  Grid: (ceil(blocks / 4), Hkv, ranges x layers).
 template <bool E4M3, bool PAGED>
 __global__ __launch_bounds__(256) void block_bounds_kernel(
     const SeqMeta* __restrict__ meta, const void* __restrict__ kpool,
     const uint8_t* __restrict__ k_scale, int8_t* __restrict__ bounds, int8_t* __restrict__ units,
-    int layer, int Hkv, Paging pg, BoundsBatch batch) {
-  const BoundsRange range = batch.r[blockIdx.z];
+    int Hkv, Paging pg, BoundsBatch batch) {
+  const BoundsRange range = batch.r[blockIdx.z % batch.n];
+  const int layer = batch.layer[blockIdx.z / batch.n];
   const int b = range.from + static_cast<int>(blockIdx.x) * 4 +
                 __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (b >= range.to) return;
@@ -192,7 +195,7 @@ void launch_choose(const Shape& sh, const SeqMeta* meta, const void* q, int laye
 }  // namespace
 
 hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void* kpool,
-                               int8_t* bounds, int64_t pool_rows, int layer,
+                               int8_t* bounds, int64_t pool_rows, const int* layers, int n_layers,
                                const BoundsRange* ranges, int n, hipStream_t s) {
   int8_t* units = bounds + pool_rows / kBlockRows * kBoundsBytes;
   const auto kernel =
@@ -200,18 +203,20 @@ hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void*
                                     : block_bounds_kernel<true, false>)
                     : (sh.pg.tables ? block_bounds_kernel<false, true>
                                     : block_bounds_kernel<false, false>);
-  for (int i0 = 0; i0 < n; i0 += kBoundsBatch) {
-    BoundsBatch b{};
-    const int k = std::min(kBoundsBatch, n - i0);
-    int most = 0;
-    for (int i = 0; i < k; ++i) {
-      b.r[i] = ranges[i0 + i];
-      most = std::max(most, b.r[i].to - b.r[i].from);
+  for (int l0 = 0; l0 < n_layers; l0 += kBoundsBatch) {
+    for (int i0 = 0; i0 < n; i0 += kBoundsBatch) {
+      BoundsBatch b{};
+      b.n = std::min(kBoundsBatch, n - i0);
+      const int nl = std::min(kBoundsBatch, n_layers - l0);
+      std::copy(ranges + i0, ranges + i0 + b.n, b.r);
+      std::copy(layers + l0, layers + l0 + nl, b.layer);
+      int most = 0;
+      for (int i = 0; i < b.n; ++i) most = std::max(most, b.r[i].to - b.r[i].from);
+      hipLaunchKernelGGL(kernel, dim3((most + 3) / 4, sh.Hkv, b.n * nl), dim3(256), 0, s, meta,
+                         kpool, sh.k_scale, bounds, units, sh.Hkv, sh.pg, b);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((most + 3) / 4, sh.Hkv, k), dim3(256), 0, s, meta, kpool,
-                       sh.k_scale, bounds, units, layer, sh.Hkv, sh.pg, b);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }

@@ -94,6 +94,7 @@ struct ra_cache {
   // per layer and slot how many leading blocks of a head they are current for
   int8_t* bounds = nullptr;
   std::vector<int32_t> bounds_built;
+  std::vector<uint8_t> sparse_layers;    // layers that sparse steps were made of
 
   ra::Shape shape() const {
     ra::Shape sh{cfg.num_layers, cfg.num_q_heads, cfg.num_kv_heads, G,

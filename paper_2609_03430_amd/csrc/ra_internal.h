@@ -279,11 +279,11 @@ __device__ __host__ inline int attended_blocks(int len, int recent, int n_blocks
 // bound of each channel, then the lower), then an int8 exponent per block.
 constexpr int kBoundsBytes = 2 * kHeadDim;
 struct BoundsRange {
-  int32_t slot, from, to;   // a slot's blocks [from, to) of every head of a layer
+  int32_t slot, from, to;   // a slot's blocks [from, to) of every head of the layers
 };
-constexpr int kBoundsBatch = 64;   // ranges per launch
+constexpr int kBoundsBatch = 64;   // ranges, and layers, per launch
 hipError_t launch_block_bounds(const Shape& sh, const SeqMeta* meta, const void* kpool,
-                               int8_t* bounds, int64_t pool_rows, int layer,
+                               int8_t* bounds, int64_t pool_rows, const int* layers, int n_layers,
                                const BoundsRange* ranges, int n, hipStream_t s);
 // Chosen blocks of the heads of the active slots below max_seqs that have more than
 // choice.n_blocks candidates and more than their attention chooses from itself

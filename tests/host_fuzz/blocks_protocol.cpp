@@ -52,7 +52,7 @@ void rows_change(int s, int from) {
 }
 
 void check_candidates(int layer, int recent, int n_blocks) {
-  for (int s = 0; s < kSlots; ++s) {
+  for (int s = 0; n_blocks > 0 && s < kSlots; ++s) {
     const ra_seq_info i = info_of(s);
     if (!i.active) continue;
     const int cand = ra::candidate_blocks(i.len, recent);
@@ -81,17 +81,21 @@ hipError_t launch_export_rows(const Shape&, const SeqMeta&, int, int, const void
 }
 
 hipError_t launch_block_bounds(const Shape&, const SeqMeta*, const void*, int8_t* bounds,
-                               int64_t pool_rows, int layer, const BoundsRange* r, int n,
-                               hipStream_t) {
+                               int64_t pool_rows, const int* layers, int n_layers,
+                               const BoundsRange* r, int n, hipStream_t) {
   ++g_launches;
+  if (n_layers < 1 || n < 1) fail("empty launch", n_layers, n);
   if (bounds != g_buf || pool_rows / 32 * (kBoundsBytes + 1) > static_cast<int64_t>(g_buf_bytes))
     fail("bounds buffer", pool_rows, static_cast<long long>(g_buf_bytes));
   for (int i = 0; i < n; ++i) {
     const ra_seq_info s = info_of(r[i].slot);
     if (!s.active || r[i].from >= r[i].to || r[i].from < 0 || 32 * r[i].to > s.len)
       fail("range", r[i].from, r[i].to);
-    for (int b = r[i].from; b < r[i].to; ++b, ++g_bounds_built)
-      g_bounds[layer][r[i].slot][b] = g_version;
+    for (int l = 0; l < n_layers; ++l) {
+      if (layers[l] < 0 || layers[l] >= L) fail("layer", layers[l], L);
+      for (int b = r[i].from; b < r[i].to; ++b, ++g_bounds_built)
+        g_bounds[layers[l]][r[i].slot][b] = g_version;
+    }
   }
   return hipSuccess;
 }
