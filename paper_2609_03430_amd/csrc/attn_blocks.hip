@@ -80,6 +80,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // ---- bf16 rows -----------------------------------------------------------------
 
 struct Bf16Rows {
+  static constexpr int kWaves = 2;    // per SIMD: up to 256 registers each
   using Block = BlockRegs;
   using Channels = RowChannels;
   struct Query {
@@ -162,6 +163,7 @@ struct E4m3Block {
 };
 
 struct E4m3Rows {
+  static constexpr int kWaves = 3;    // per SIMD: up to 168 registers each
   using Block = E4m3Block;
   struct Channels {
     static __device__ __forceinline__ int first(int u, int grp) {
@@ -171,48 +173,52 @@ struct E4m3Rows {
 
   // S^T comes from the codes themselves (v_mfma_scale_f32_16x16x128_f8f6f4, the rows'
   // scale bytes its operands' scales), so the query has to be in 8 bits too: it is
-  // the sum of two E4M3 rows, hi = E4M3(q / 2^s) and lo = E4M3(16 (q / 2^s - hi)).
-  // A bf16 value has 8 significant bits, hi the first four and lo the others, so the
-  // sum is exact where |q_c| is at least 2^-14 of the row's largest, and below it is
-  // off by at most 2^-22 of the largest: the size of the products' fp32 rounding.
-  // (16 products of 16x16x128 per 128 keys, where converting the keys to bf16 took as
-  // many matrix cycles and 32 to 64 vector instructions per 32 keys.)
+  // the sum of three E4M3 rows, each the rounding of 16 times what the one before left
+  // (its scale 2^-4 of that one's).  A bf16 value has 8 significant bits and a part takes
+  // four, so two parts hold it where |q_c| is at least 2^-14 of the row's largest; the
+  // third brings that to 2^-18 and the error below to 2^-26 of the largest, under the
+  // rounding of the products' sum in fp32 (two parts, 2^-22, are no faster: 256 heads of
+  // 9,000 rows 105 us, 8 of 2,200 10.4, both ways).
+  // Six products of 16x16x128 per block of 32 keys take 192 cycles, the eight of
+  // 16x16x32 that bf16 keys need 128, but none of the instructions of a conversion.
   struct Query {
-    i32x8 hi, lo;
-    int scale_hi, scale_lo;
+    static constexpr int kParts = 3;
+    i32x8 part[kParts];
+    int scale;                       // byte n: part n's, 4 less than the part's before
     static __device__ __forceinline__ int channel(int i, int grp) {
       return 64 * (i >> 1) + 16 * grp + 8 * (i & 1);
     }
     __device__ __forceinline__ void set(const u32x4 (&raw)[4], bool real) {
-      float x[32];
       uint32_t amax = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t u = real ? raw[i][j] : 0u;
-          x[8 * i + 2 * j] = bf16_low(u);
-          x[8 * i + 2 * j + 1] = bf16_high(u);
-          amax = max(amax, max(row_magnitude(bf16_low(u)), row_magnitude(bf16_high(u))));
-        }
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t u = real ? raw[i >> 2][i & 3] : 0u;
+        amax = max(amax, max(row_magnitude(bf16_low(u)), row_magnitude(bf16_high(u))));
       }
-      const uint32_t byte = max(e4m3_scale_byte(max_over_groups(amax)), 5u);   // lo's: 4 less
+      const uint32_t byte =
+          max(e4m3_scale_byte(max_over_groups(amax)), 4u * (kParts - 1) + 1u);
       const float inv = e4m3_inverse(byte);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = e4m3_clamp(x[i] * inv, byte);
+      for (int i = 0; i < 8; ++i) {                      // four channels at a time
+        float x[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t h = e4m3_pack2<true>(x[4 * i + 2], x[4 * i + 3],
-                                            e4m3_pack2<false>(x[4 * i], x[4 * i + 1], 0u));
-        const f32x2 a = e4m3_unpack2<false>(h), b = e4m3_unpack2<true>(h);
-        const uint32_t l = e4m3_pack2<true>(
-            16.f * (x[4 * i + 2] - b[0]), 16.f * (x[4 * i + 3] - b[1]),
-            e4m3_pack2<false>(16.f * (x[4 * i] - a[0]), 16.f * (x[4 * i + 1] - a[1]), 0u));
-        hi[i] = static_cast<int>(h);
-        lo[i] = static_cast<int>(l);
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t u = real ? raw[i >> 1][2 * (i & 1) + j] : 0u;
+          x[2 * j] = e4m3_clamp(bf16_low(u) * inv, byte);
+          x[2 * j + 1] = e4m3_clamp(bf16_high(u) * inv, byte);
+        }
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) {
+          const uint32_t c = e4m3_pack2<true>(x[2], x[3], e4m3_pack2<false>(x[0], x[1], 0u));
+          part[n][i] = static_cast<int>(c);
+          const f32x2 lo = e4m3_unpack2<false>(c), hi = e4m3_unpack2<true>(c);
+          x[0] = 16.f * (x[0] - lo[0]);
+          x[1] = 16.f * (x[1] - lo[1]);
+          x[2] = 16.f * (x[2] - hi[0]);
+          x[3] = 16.f * (x[3] - hi[1]);
+        }
       }
-      scale_hi = static_cast<int>(byte);
-      scale_lo = static_cast<int>(byte - 4);
+      scale = static_cast<int>(byte | (byte - 4) << 8 | (byte - 8) << 16);
     }
   };
 
@@ -320,14 +326,16 @@ struct E4m3Rows {
     f32x4 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const f32x4 z = {0.f, 0.f, 0.f, 0.f};
       i32x8 k;
       __builtin_memcpy(&k, b.k[t], 32);
       const int scale = static_cast<int>(static_cast<uint32_t>(b.ks >> (32 * t)) >> key_shift());
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.lo, z, 0, 0, 0, scale, 0,
-                                                              q.scale_lo);
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.hi, s[t], 0, 0, 0, scale, 0,
-                                                              q.scale_hi);
+      const f32x4 z = {0.f, 0.f, 0.f, 0.f};              // the smallest part first
+      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[2], z, 0, 0, 0, scale, 2,
+                                                              q.scale);
+      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[1], s[t], 0, 0, 0, scale,
+                                                              1, q.scale);
+      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[0], s[t], 0, 0, 0, scale,
+                                                              0, q.scale);
     }
     const int grp = (threadIdx.x & 63) >> 4;
     float x[8];
@@ -382,6 +390,15 @@ struct E4m3Rows {
   }
 };
 
+// W wavefronts (four) per workgroup, two register buffers of a block each (three and
+// four, and eight or twelve wavefronts, measured no faster), within 168 registers for
+// e4m3 rows, so that three workgroups fit a CU.  Bound by HBM where the rows are many:
+// 256 heads of 9,216 e4m3 rows 95 us (6.4 TB/s; of 8,250 in a decode window 90 us, where
+// the bf16 launch takes 174), 256 heads attending to 40 of 288 bf16 blocks 28 us
+// (5.9 TB/s) and 8 us for the choice.  Bound by latency where they are few: 8 heads of
+// 2,200 rows 9.9 us (slot record, rows, partials out, counter, partials in), two of 200
+// 6.0.  The keys' scores on scaled products and two values converted at a time took
+// the first of these from 117 us to 98.
 template <typename R, int W, int MINW, bool PAGED, bool LIST>
 __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
     AttnLaunch a, BlockChoice ch, SlotOrder order, Paging pg, uint8_t* k_scale, uint8_t* v_scale,
@@ -515,8 +532,8 @@ void launch_blocks(const Shape& sh, const AttnLaunch& a, const BlockChoice& ch, 
   const SlotOrder order = sh.order ? *sh.order : SlotOrder{};
   const dim3 grid(a.max_splits, sh.Hkv, order.n ? order.n : a.max_seqs);
   const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(kHeadDim));
-  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, 2, PAGED, LIST>), grid, dim3(256), 0, s, a, ch,
-                     order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
+  hipLaunchKernelGGL((attn_blocks_kernel<R, 4, R::kWaves, PAGED, LIST>), grid, dim3(256), 0, s, a,
+                     ch, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv, scale_log2);
 }
 
 }  // namespace

@@ -334,3 +334,31 @@ def test_random_configurations():
             check_step(run, oracles, outs, (trial, t))
         check_heads(run, oracles)
         run.close()
+
+
+@pytest.mark.parametrize("ratio", [1, 2.0 ** 10, 2.0 ** 14])
+def test_a_channel_that_dwarfs_the_query(ratio):
+    """One channel of the query, 4 * `ratio`, dwarfs the others, of size 1, and no key has
+    it: the scores come from the others alone.  The query's parts hold every channel to
+    2^-26 of the largest, so a score is off by at most 127 * 2 * 2^-26 * 4 ratio /
+    sqrt(128) (|k| <= 2), a weight by e to the power of twice that, an output (|v| <= 2)
+    by 4 times its distance from 1."""
+    n = 700
+    c = _cache(1, 4, 1, [n])
+    g = torch.Generator().manual_seed(int(ratio))
+    k, v = (torch.randn(1, 1, n, 128, generator=g).clamp(-2, 2).to(torch.bfloat16) for _ in range(2))
+    k[..., 5] = 0
+    B.ra_seq_begin(c.handle, 0, n, 1, 0, k.to(DEV), v.to(DEV))
+    q = torch.randn(1, 4, 128, generator=g).to(torch.bfloat16)
+    q[..., 5] = ratio * 4
+    kn, vn = (torch.randn(1, 1, 128, generator=g).clamp(-2, 2).to(torch.bfloat16) for _ in range(2))
+    kn[..., 5] = 0
+    out = torch.empty_like(q, device=DEV)
+    c.decode(0, q.to(DEV), kn.to(DEV), vn.to(DEV), out)
+    K = torch.cat([held(k)[0, 0], held(kn)[0]]).double().numpy()
+    V = torch.cat([held(v)[0, 0], held(vn)[0]]).double().numpy()
+    want = gqa_decode(q[0].double().numpy(), [K], [V])
+    slack = 2 * 2 * np.expm1(2 * 127 * 2 * 2.0 ** -26 * 4 * ratio / np.sqrt(128))
+    err = np.abs(out[0].double().cpu().numpy() - want)
+    assert (err <= 2.0 ** -8 * np.abs(want) + 1e-4 + slack).all(), (ratio, err.max(), slack)
+    c.close()
