@@ -31,7 +31,7 @@
  *   error leaves device state untouched.  A failed launch returns
  *   RA_ERR_HIP (ra_last_hip_error gives the hipError_t); after RA_ERR_HIP
  *   from a call that launches several kernels (ra_seq_begin, a paged or
- *   move-carrying ra_decode_attention, ra_end_step, ra_evict_now,
+ *   move-carrying ra_decode_attention, ra_sparse_attention, ra_end_step, ra_evict_now,
  *   ra_fast_forward, ra_seq_fast_forward, ra_scored_evict) the host mirror
  *   and the device state may disagree, and the cache should be destroyed.
  *   Nothing throws across the ABI.

@@ -501,8 +501,8 @@ def ra_sparse_attention(handle, layer, n_blocks, recent_rows, q, k_new, v_new, o
     _arg(workspace, "ra_sparse_attention", "workspace")
     _check(_lib().ra_sparse_attention(handle, int(layer), int(n_blocks), int(recent_rows),
                                       _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
-                                      _ptr(workspace), _bytes(workspace), _stream(stream)),
-           "ra_sparse_attention")
+                                      _ptr(workspace), 0 if workspace is None else _bytes(workspace),
+                                      _stream(stream)), "ra_sparse_attention")
 
 
 def ra_attention_plan(handle):
@@ -540,6 +540,7 @@ class Cache:
         self.meta = torch.zeros(ra_meta_bytes(cfg), dtype=torch.uint8, device=self.device)
         self.workspace = torch.empty(ra_workspace_bytes(cfg), dtype=torch.uint8,
                                      device=self.device)
+        self.bounds = self.sparse_workspace = None       # (attach_sparse)
         self.handle = ra_cache_create(cfg, self.k_pool, self.v_pool, self.pos_pool,
                                       pool_rows, self.meta, stream)
 
@@ -562,7 +563,8 @@ class Cache:
         ra_decode_attention_noalloc(self.handle, layer, q, k_new, v_new, out, stream)
 
     def attach_sparse(self, n_blocks, stream=None):
-        """Bounds and workspace for sparse steps of up to n_blocks blocks per head."""
+        """Bounds and workspace for sparse steps of up to n_blocks blocks per head (the
+        bounds attached before are computed anew)."""
         size = ra_sparse_bytes(self.cfg, self.pool_rows)
         if size == 0:
             raise RandAttnError(RA_ERR_UNSUPPORTED, "ra_sparse_bytes")

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <new>
 #include <vector>
 
 #include "cache.h"
@@ -71,10 +72,18 @@ ra_status ra_sparse_attach(ra_cache* c, void* bounds, size_t bounds_bytes, void*
   if (c->graph || c->step_open()) return RA_ERR_STATE;
   const ra_status fl = ra::host::flush_pending(c, static_cast<hipStream_t>(stream));
   if (fl != RA_OK) return fl;
+  try {
+    std::vector<int32_t> built(
+        bounds ? static_cast<size_t>(c->cfg.num_layers) * c->cfg.max_seqs : 0, 0);
+    std::vector<uint8_t> layers(c->cfg.num_layers, 0);
+    c->ranges.reserve(c->cfg.max_seqs);
+    c->stale_layers.reserve(c->cfg.num_layers);
+    c->bounds_built.swap(built);
+    c->sparse_layers.swap(layers);
+  } catch (const std::bad_alloc&) {
+    return RA_ERR_CAPACITY;
+  }
   c->bounds = static_cast<int8_t*>(bounds);
-  c->bounds_built.assign(
-      bounds ? static_cast<size_t>(c->cfg.num_layers) * c->cfg.max_seqs : 0, 0);
-  c->sparse_layers.assign(c->cfg.num_layers, 0);
   return RA_OK;
 }
 
@@ -91,11 +100,16 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
     return RA_ERR_INVALID_ARG;
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   // what to rebuild is decided here: a replay would not decide it again
+  // (nor may the null stream be used while another is captured)
   hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
-  RA_LAUNCH(hipStreamIsCapturing(hs, &capturing));
+  const hipError_t asked = hipStreamIsCapturing(hs, &capturing);
+  if (asked != hipSuccess) (void)hipGetLastError();   // (the next launch must not report it)
+  if (asked == hipErrorStreamCaptureImplicit) return RA_ERR_STATE;
+  if (asked != hipSuccess) return ra::host::hip_fail(asked);
   if (capturing != hipStreamCaptureStatusNone) return RA_ERR_STATE;
   // the attended rows of the longest step, and the slots that choose their blocks
-  std::vector<ra::BoundsRange> ranges;
+  std::vector<ra::BoundsRange>& ranges = c->ranges;
+  ranges.clear();
   int most = 0, n_active = 0, candidates = 0;
   bool stale = false;
   const auto built = [&](int l, int s) -> int32_t& {
@@ -123,7 +137,8 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
     // one launch for every layer that sparse steps are made of: rows change in all
     // layers at once (36 layers of a request of 2,100 rows, one launch each: 4.8 us
     // each)
-    std::vector<int> layers;
+    std::vector<int>& layers = c->stale_layers;
+    layers.clear();
     for (int l = 0; l < c->cfg.num_layers; ++l) {
       bool any = false;
       for (ra::BoundsRange& r : ranges) {

@@ -95,6 +95,8 @@ struct ra_cache {
   int8_t* bounds = nullptr;
   std::vector<int32_t> bounds_built;
   std::vector<uint8_t> sparse_layers;    // layers that sparse steps were made of
+  std::vector<ra::BoundsRange> ranges;   // a step's own, room for every slot and layer
+  std::vector<int> stale_layers;         //   set aside when bounds are attached
 
   ra::Shape shape() const {
     ra::Shape sh{cfg.num_layers, cfg.num_q_heads, cfg.num_kv_heads, G,

@@ -11,6 +11,7 @@
 // Usage: blocks_protocol SEED DTYPE LAYOUT OPS
 #include <cstdio>
 #include <cstdlib>
+#include <new>
 #include <random>
 #include <vector>
 
@@ -28,7 +29,8 @@ int64_t g_version = 1;
 int64_t g_rows[kSlots][kRowsMax];                  // version of each row of a slot
 int64_t g_bounds[L][kSlots][kRowsMax / 32];        // version a block's bounds are of
 ra_cache* g_cache = nullptr;
-bool g_capturing = false;
+bool g_capturing = false, g_implicit = false, g_no_memory = false;
+int g_hip_error = 0;                               // what hipGetLastError would report
 int g_launches = 0, g_bounds_built = 0, g_checked = 0;
 char* g_ws = nullptr;
 size_t g_ws_bytes = 0;
@@ -67,7 +69,27 @@ void check_candidates(int layer, int recent, int n_blocks) {
 
 }  // namespace
 
+// host memory that runs out while g_no_memory is set
+void* operator new(size_t n) {
+  void* p = g_no_memory ? nullptr : std::malloc(n ? n : 1);
+  if (!p) throw std::bad_alloc();
+  return p;
+}
+void* operator new(size_t n, const std::nothrow_t&) noexcept { return std::malloc(n ? n : 1); }
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
+
+extern "C" hipError_t hipGetLastError() {
+  const int e = g_hip_error;
+  g_hip_error = 0;
+  return static_cast<hipError_t>(e);
+}
+
 extern "C" hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* out) {
+  if (g_implicit) {                                  // another stream is captured
+    g_hip_error = hipErrorStreamCaptureImplicit;
+    return hipErrorStreamCaptureImplicit;
+  }
   *out = g_capturing ? hipStreamCaptureStatusActive : hipStreamCaptureStatusNone;
   return hipSuccess;
 }
@@ -204,7 +226,14 @@ int main(int argc, char** argv) {
         break;
       case 5: {
         const bool detach = pick(6) == 0;
+        g_no_memory = pick(4) == 0;
         st = ra_sparse_attach(g_cache, detach ? nullptr : g_buf, g_buf_bytes, nullptr);
+        const bool tried = g_no_memory && !graph;
+        g_no_memory = false;
+        if (tried) {
+          if (st != RA_ERR_CAPACITY) fail("attach without memory", st, detach);
+          break;                                     // what was attached stays
+        }
         if (st != (graph ? RA_ERR_STATE : RA_OK)) fail("attach", st, graph);
         if (st == RA_OK) {
           attached = !detach;
@@ -237,11 +266,14 @@ int main(int argc, char** argv) {
           const bool want = pick(3) != 0;
           const int mark = g_launches;
           g_capturing = pick(20) == 0;
+          g_implicit = pick(20) == 0;
+          g_no_memory = c.layout != RA_LAYOUT_PAGED;   // (new pages extend the tables)
           st = want ? ra_sparse_attention(g_cache, l, n_blocks, recent, q.data(), kv.data(),
                                           kv.data(), q.data(), g_ws, g_ws_bytes, nullptr)
                     : RA_ERR_STATE;
-          const bool may = attached && !graph && !g_capturing;
-          g_capturing = false;
+          const bool may = attached && !graph && !g_capturing && !g_implicit;
+          g_capturing = g_implicit = g_no_memory = false;
+          if (hipGetLastError() != hipSuccess) fail("an error is left behind", l, st);
           if (want && st != RA_OK) {
             if (st == RA_ERR_STATE ? may : st != RA_ERR_CAPACITY) fail("sparse", st, may);
             if (g_launches != mark) fail("launched and refused", st, l);
