@@ -115,6 +115,28 @@ def test_equal_scores_take_the_lowest_blocks(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_equal_scores_of_long_heads(dtype):
+    """Heads that a launch of its own chooses from: every score the same, every score 0,
+    two scores, and scores of both signs."""
+    lens = [17000, 36000]
+    keys, values, q, kn, vn = _inputs(7, lens, 4, 2)
+    for k in keys:
+        k[:, 32:] = k[:, :32].repeat(1, k.shape[1] // 32 + 1, 1)[:, :k.shape[1] - 32]
+    f = Fixed(dtype, 4, 2, keys, values)
+    f.check(7, 20, q, kn, vn)
+    q[:] = 0
+    f.check(7, 20, q, kn, vn)
+    f.close()
+    keys, values, q, kn, vn = _inputs(8, lens, 4, 2)
+    for k in keys:
+        k[:, 32:] = k[:, :32].repeat(1, k.shape[1] // 32 + 1, 1)[:, :k.shape[1] - 32]
+        k[:, 320:] *= -1
+    f = Fixed(dtype, 4, 2, keys, values)
+    f.check(13, 20, q, kn, vn)
+    f.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
 def test_extreme_scales(dtype):
     """Exponents outside the scores' range, signs of one kind, zero keys."""
     keys, values, q, kn, vn = _inputs(6, [600, 600, 600], 6, 2)
