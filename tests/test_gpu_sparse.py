@@ -115,6 +115,26 @@ def test_equal_scores_take_the_lowest_blocks(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_keys_below_the_smallest_normal(dtype):
+    """Bounds of magnitudes under 2^-126: any positive one rounds up to 2^-60, any
+    negative one down to -2^-60, and zeros stay."""
+    keys, values, q, kn, vn = _inputs(9, [900, 1300], 4, 2)
+    for i, k in enumerate(keys):
+        g = torch.Generator().manual_seed(90 + i)
+        k *= (torch.rand(k.shape, generator=g) < 0.02) * 2.0 ** -128
+        k[0] = k[0].abs()
+    f = Fixed(dtype, 4, 2, keys, values)
+    for n_blocks in (1, 7):
+        _, lists = f.step(n_blocks, 20, q, kn, vn)
+        for i, n in enumerate((900, 1300)):
+            for g in range(2):
+                want = blocks.chosen(q[i, 2 * g:2 * g + 2].double().numpy(),
+                                     f.k[i][g].double().numpy(), n, n_blocks, 20)
+                assert np.array_equal(lists[i, g], want), (i, g, n_blocks)
+    f.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
 def test_equal_scores_of_long_heads(dtype):
     """Heads that a launch of its own chooses from: every score the same, every score 0,
     two scores, and scores of both signs."""
