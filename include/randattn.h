@@ -91,7 +91,8 @@ typedef enum {
                   the largest bf16 number; a NaN stays one and does not count
                   in amax.  What is read back is exactly what the codes stand
                   for, writing it again gives the same values, and attention
-                  attends to these values, the new pair's included.  Not with
+                  attends to these values, the new pair's included (an infinite
+                  query channel counts as the largest bf16 number, too).  Not with
                   RA_LAYOUT_HOLE_FILL, ra_window_select or ra_scored_evict
                   (RA_ERR_UNSUPPORTED). */
 } ra_dtype;

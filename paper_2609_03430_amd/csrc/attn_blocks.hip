@@ -198,14 +198,15 @@ struct E4m3Rows {
       const uint32_t byte =
           max(e4m3_scale_byte(max_over_groups(amax)), 4u * (kParts - 1) + 1u);
       const float inv = e4m3_inverse(byte);
+      const float top = byte < 247u ? 448.f : 255.f;     // 255 * 2^120: the largest bf16
 #pragma unroll
       for (int i = 0; i < 8; ++i) {                      // four channels at a time
         float x[4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint32_t u = real ? raw[i >> 1][2 * (i & 1) + j] : 0u;
-          x[2 * j] = e4m3_clamp(bf16_low(u) * inv, byte);
-          x[2 * j + 1] = e4m3_clamp(bf16_high(u) * inv, byte);
+          x[2 * j] = within(bf16_low(u) * inv, top);
+          x[2 * j + 1] = within(bf16_high(u) * inv, top);
         }
 #pragma unroll
         for (int n = 0; n < kParts; ++n) {

@@ -77,12 +77,15 @@ __device__ __forceinline__ float e4m3_inverse(uint32_t byte) {
   return __uint_as_float((254u - byte) << 23);
 }
 
-// x divided by the row's scale, within the codes' range (comparisons that a NaN
-// fails, so that it reaches the conversion).
-__device__ __forceinline__ float e4m3_clamp(float y, uint32_t byte) {
-  const float limit = byte < 247u ? 448.f : 240.f;
+// y within +-limit (comparisons that a NaN fails, so that it stays one).
+__device__ __forceinline__ float within(float y, float limit) {
   y = y > limit ? limit : y;
   return y < -limit ? -limit : y;
+}
+
+// x divided by the row's scale, within the codes' range.
+__device__ __forceinline__ float e4m3_clamp(float y, uint32_t byte) {
+  return within(y, byte < 247u ? 448.f : 240.f);
 }
 
 // The codes of x and y (divided by the scale and clamped) in the low 16 bits of the

@@ -362,3 +362,33 @@ def test_a_channel_that_dwarfs_the_query(ratio):
     err = np.abs(out[0].double().cpu().numpy() - want)
     assert (err <= 2.0 ** -8 * np.abs(want) + 1e-4 + slack).all(), (ratio, err.max(), slack)
     c.close()
+
+
+@pytest.mark.parametrize("top", ["largest", "infinite"])
+def test_the_largest_queries(top):
+    """A query channel of the largest bf16 number, 255 * 2^120, which the codes of a cached
+    row would not reach, or infinite, which counts as that: against keys of 2^-126 to 2^-122 the
+    scores are up to 64 / sqrt(128), and as exact as others."""
+    n = 500
+    largest = 255 * 2.0 ** 120
+    c = _cache(1, 2, 1, [n])
+    g = torch.Generator().manual_seed(12)
+    k = torch.zeros(1, 1, n + 1, 128)
+    k[..., 7] = (torch.rand(1, 1, n + 1, generator=g) * 32 - 16).round() * 2.0 ** -126
+    k = k.to(torch.bfloat16)
+    v = torch.randn(1, 1, n + 1, 128, generator=g).clamp(-2, 2).to(torch.bfloat16)
+    q = torch.zeros(1, 2, 128)
+    q[0, 0, 7], q[0, 1, 7] = largest, -largest
+    want = gqa_decode(q[0].double().numpy(), [held(k)[0, 0].double().numpy()],
+                      [held(v)[0, 0].double().numpy()])
+    if top == "infinite":
+        q *= float("inf")
+        q[q.isnan()] = 0
+    B.ra_seq_begin(c.handle, 0, n, 1, 0, k[:, :, :n].contiguous().to(DEV),
+                   v[:, :, :n].contiguous().to(DEV))
+    out = torch.empty(1, 2, 128, dtype=torch.bfloat16, device=DEV)
+    c.decode(0, q.to(torch.bfloat16).to(DEV), k[:, :, n].contiguous().to(DEV),
+             v[:, :, n].contiguous().to(DEV), out)
+    err = np.abs(out[0].double().cpu().numpy() - want)
+    assert (err <= 2.0 ** -8 * np.abs(want) + 1e-4).all(), err.max()
+    c.close()
