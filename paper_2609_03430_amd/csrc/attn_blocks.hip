@@ -394,12 +394,11 @@ struct E4m3Rows {
 // W wavefronts (four) per workgroup, two register buffers of a block each (three and
 // four, and eight or twelve wavefronts, measured no faster), within 168 registers for
 // e4m3 rows, so that three workgroups fit a CU.  Bound by HBM where the rows are many:
-// 256 heads of 9,216 e4m3 rows 95 us (6.4 TB/s; of 8,250 in a decode window 90 us, where
-// the bf16 launch takes 174), 256 heads attending to 40 of 288 bf16 blocks 28 us
-// (5.9 TB/s) and 8 us for the choice.  Bound by latency where they are few: 8 heads of
-// 2,200 rows 9.9 us (slot record, rows, partials out, counter, partials in), two of 200
-// 6.0.  The keys' scores on scaled products and two values converted at a time took
-// the first of these from 117 us to 98.
+// 256 heads of 9,216 e4m3 rows 95 to 100 us (6.1 to 6.4 TB/s; 117 with the keys converted
+// to bf16 and the values one at a time), of 8,250 in a decode window 90 us, where the
+// bf16 launch takes 174; 256 heads attending to 38 of 288 bf16 blocks 28 us (5.7 TB/s) and 8
+// us for the choice.  Bound by latency where they are few: 8 heads of 2,200 rows 10.0 us
+// (slot record, rows, partials out, counter, partials in), two of 200 6.5.
 template <typename R, int W, int MINW, bool PAGED, bool LIST>
 __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
     AttnLaunch a, BlockChoice ch, SlotOrder order, Paging pg, uint8_t* k_scale, uint8_t* v_scale,
