@@ -895,6 +895,7 @@ ra_status ra_end_step(ra_cache* c, void* stream, int32_t* n_evicted) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   std::fill(c->appended.begin(), c->appended.end(), 0);
   c->n_appended = 0;
+  c->order_sorted = false;
   if (!any_active) return RA_OK;
   RA_LAUNCH(ra::launch_advance(c->meta, c->slot_lo, c->slot_hi, 1, c->cfg.recent_r,
                                trigger_every(c->cfg), s));

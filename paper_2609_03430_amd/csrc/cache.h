@@ -111,14 +111,16 @@ struct ra_cache {
   // attention over blocks: the active slots, the longest first (see refresh_order)
   ra::SlotOrder order;
   bool order_stale = true;               // the active slots changed
+  bool order_sorted = false;             // sorted by the lengths of this step
 
-  // Brings `order` up to date, at the first layer of a step, and returns it where the
-  // caches are ragged: heads that start last should be short (microseconds per step,
+  // Brings `order` up to date, at the first launch of a step that asks for it (not
+  // the first layer: launches that take no order may come before), and returns it where
+  // the caches are ragged: heads that start last should be short (microseconds per step,
   // slots as they come and the longest first: 1,280 heads of 1,000 to 9,000 e4m3 rows 340
   // and 289, 480 paged ones of 300 to 4,100 76 and 68).  Lengths hardly change their
   // order between steps, so an insertion sort goes over them once.
   const ra::SlotOrder* refresh_order() {
-    if (n_appended == 0) {
+    if (n_appended == 0 || order_stale || !order_sorted) {
       if (order_stale) {
         order.n = 0;
         int active = 0;
@@ -136,6 +138,7 @@ struct ra_cache {
           order.slot[j] = order.slot[j - 1];
         order.slot[j] = s;
       }
+      order_sorted = true;
     }
     if (order.n < 2) return nullptr;
     const int longest = mirror[order.slot[0]].len, shortest = mirror[order.slot[order.n - 1]].len;
