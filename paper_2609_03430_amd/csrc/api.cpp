@@ -275,20 +275,21 @@ int mid_plan(const ra_cache* c, Plan& p, int heads, int keys_max, int64_t keys_m
 
 // Attention over blocks of rows (attn_blocks.hip): `heads` heads of up to keys_max
 // attended rows, workgroups of four wavefronts, three of which fit a CU.  Measured with
-// e4m3 rows and G = 5 (microseconds per step, splits of a head: time):
+// e4m3 rows, every one attended, and G = 5 (microseconds per layer in a captured step of
+// 2 to 48 layers, its end included; splits of a head: time):
 //   up to 256 heads, as many splits as leave no CU two workgroups: 96 heads of 9,000 keys
-//     2: 46, 3: 59; 64 heads 4: 33, 8: 36; 192 heads 1: 84, 2: 96;
+//     2: 47, 3: 60; 64 heads 4: 35, 8: 37; 192 heads 1: 88, 2: 99;
 //   no fewer than 256 keys to a workgroup (past 64 heads 512), half as many again
-//     staying whole: 8 heads of 300 keys 1: 7.5, 2: 8.4; of 2,200 9: 10.3, 14: 11.3; 128
-//     heads of 600 1: 13.4, 2: 14.6;
+//     staying whole: 8 heads of 300 keys 1: 7.1, 2: 7.8; of 2,200 9: 9.7, 14: 10.6; 128
+//     heads of 600 1: 13.5, 2: 14.7;
 //   past 12 splits the merge of one more costs 0.4, a workgroup 1,000 keys 5.7: 8 heads of
-//     9,000 keys 12: 14.4, 32: 17.2; of 30,000 12: 25.5, 24: 23.0, 32: 22.6;
+//     9,000 keys 12: 14.4, 32: 17.0; of 30,000 12: 26.1, 24: 23.0, 30: 22.5, 32: 22.7;
 //   between 256 and 768 heads, long ones are split where that evens out the CUs' load:
-//     of 9,000 keys, 264 heads 1: 160, 2: 141, 3: 133, 6: 128; 320 1: 166, 2: 148, 3: 140;
-//     384 1: 178, 2: 162, 3: 168; 512 1: 208, 2: 211; 640 1: 276, 2: 265; of 2,200, 264
-//     heads 1: 47, 3: 44; 320 1: 50, 3: 52; 640 1: 88, 2: 95.
+//     of 9,000 keys, 264 heads 1: 161, 2: 142, 3: 135, 6: 131; 320 1: 166, 2: 152, 3: 144;
+//     384 1: 180, 2: 166, 3: 174; 512 1: 209, 2: 217; 640 1: 280, 2: 268; of 2,200, 264
+//     heads 1: 48, 3: 44; 320 1: 52, 3: 52; 640 1: 87, 2: 94.
 // The partials of heads past 256 must fit the no-alloc entry point's array, which whole
-// heads do not need.
+// heads do not need (one plan serves all entry points).
 Plan ra::host::plan_blocks(const ra_cache* c, int64_t keys_max, int heads) {
   int64_t splits = 1;
   const int64_t unit = heads > 64 ? 512 : 256;

@@ -149,7 +149,6 @@ struct Bf16Rows {
 
 // ---- e4m3 rows -------------------------------------------------------------------
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // A lane's 16-byte loads hold 16 channels of a key row, and two channels of a value
@@ -171,55 +170,25 @@ struct E4m3Rows {
     }
   };
 
-  // S^T comes from the codes themselves (v_mfma_scale_f32_16x16x128_f8f6f4, the rows'
-  // scale bytes its operands' scales), so the query has to be in 8 bits too: it is
-  // the sum of three E4M3 rows, each the rounding of 16 times what the one before left
-  // (its scale 2^-4 of that one's).  A bf16 value has 8 significant bits and a part takes
-  // four, so two parts hold it where |q_c| is at least 2^-14 of the row's largest; the
-  // third brings that to 2^-18 and the error below to 2^-26 of the largest, under the
-  // rounding of the products' sum in fp32 (two parts, 2^-22, are no faster: 256 heads of
-  // 9,000 rows 105 us, 8 of 2,200 10.4, both ways).
-  // Six products of 16x16x128 per block of 32 keys take 192 cycles, the eight of
-  // 16x16x32 that bf16 keys need 128, but none of the instructions of a conversion.
+  // The query as it is, but for infinities, which count as the largest bf16 number.
   struct Query {
-    static constexpr int kParts = 3;
-    i32x8 part[kParts];
-    int scale;                       // byte n: part n's, 4 less than the part's before
+    bf16x8 q[4];
     static __device__ __forceinline__ int channel(int i, int grp) {
       return 64 * (i >> 1) + 16 * grp + 8 * (i & 1);
     }
     __device__ __forceinline__ void set(const u32x4 (&raw)[4], bool real) {
-      uint32_t amax = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t u = real ? raw[i >> 2][i & 3] : 0u;
-        amax = max(amax, max(row_magnitude(bf16_low(u)), row_magnitude(bf16_high(u))));
-      }
-      const uint32_t byte =
-          max(e4m3_scale_byte(max_over_groups(amax)), 4u * (kParts - 1) + 1u);
-      const float inv = e4m3_inverse(byte);
-      const float top = byte < 247u ? 448.f : 255.f;     // 255 * 2^120: the largest bf16
+      for (int s = 0; s < 4; ++s) {
+        u32x4 w;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {                      // four channels at a time
-        float x[4];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t u = real ? raw[i >> 1][2 * (i & 1) + j] : 0u;
-          x[2 * j] = within(bf16_low(u) * inv, top);
-          x[2 * j + 1] = within(bf16_high(u) * inv, top);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t u = real ? raw[s][i] : 0u;
+          if ((u & 0x7fffu) == 0x7f80u) u -= 1u;
+          if ((u & 0x7fff0000u) == 0x7f800000u) u -= 0x10000u;
+          w[i] = u;
         }
-#pragma unroll
-        for (int n = 0; n < kParts; ++n) {
-          const uint32_t c = e4m3_pack2<true>(x[2], x[3], e4m3_pack2<false>(x[0], x[1], 0u));
-          part[n][i] = static_cast<int>(c);
-          const f32x2 lo = e4m3_unpack2<false>(c), hi = e4m3_unpack2<true>(c);
-          x[0] = 16.f * (x[0] - lo[0]);
-          x[1] = 16.f * (x[1] - lo[1]);
-          x[2] = 16.f * (x[2] - hi[0]);
-          x[3] = 16.f * (x[3] - hi[1]);
-        }
+        q[s] = as_bf16x8(w);
       }
-      scale = static_cast<int>(byte | (byte - 4) << 8 | (byte - 8) << 16);
     }
   };
 
@@ -307,36 +276,41 @@ struct E4m3Rows {
     }
   };
 
-  // Eight codes as bf16 numbers.
-  static __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1) {
+  // Eight codes times a power of two as bf16 numbers.
+  static __device__ __forceinline__ bf16x8 to_bf16(uint32_t w0, uint32_t w1, float scale) {
     union {
       bf16x2 h[4];
       bf16x8 v;
     } r;
-    r.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false);
-    r.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true);
-    r.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false);
-    r.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true);
+    r.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false);
+    r.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
+    r.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false);
+    r.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
     return r.v;
   }
 
-  // compute_block over the values that the rows stand for: a key's scale goes with
-  // its codes, a value's with its weight.
+  // compute_block over the values that the rows stand for, which bf16 holds: a key's
+  // scale goes into its conversion, a value's into its weight.
+  // The scores take bf16 products, not the matrix cores' 8-bit ones (with the query in
+  // three E4M3 parts), since those cut the products of a group off about 2^-12 below the
+  // largest: sums of 128 random ones were off by up to 2.9e-4 of the largest product (bf16
+  // products 7e-7), the weights of equal scores by up to 7e-4.  Nor were they faster
+  // (microseconds per layer in a graph, 8-bit products and these: 2 heads of 200 rows 6.4
+  // and 5.7, 8 of 2,200 10.5 and 9.7, 64 of 9,000 34.9 and 34.6, 512 of 9,000 209 both).
   static __device__ __forceinline__ void compute(Softmax& st, const Block& b, const Query& q,
                                                  float scale_log2, int limit) {
     f32x4 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      i32x8 k;
-      __builtin_memcpy(&k, b.k[t], 32);
-      const int scale = static_cast<int>(static_cast<uint32_t>(b.ks >> (32 * t)) >> key_shift());
-      const f32x4 z = {0.f, 0.f, 0.f, 0.f};              // the smallest part first
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[2], z, 0, 0, 0, scale, 2,
-                                                              q.scale);
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[1], s[t], 0, 0, 0, scale,
-                                                              1, q.scale);
-      s[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[0], s[t], 0, 0, 0, scale,
-                                                              0, q.scale);
+      const float scale =
+          e4m3_scale(static_cast<uint32_t>(b.ks >> (32 * t)) >> key_shift() & 255u);
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x4 w = b.k[t][i >> 1];
+        const bf16x8 k = i & 1 ? to_bf16(w.z, w.w, scale) : to_bf16(w.x, w.y, scale);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q.q[i], s[t], 0, 0, 0);
+      }
     }
     const int grp = (threadIdx.x & 63) >> 4;
     float x[8];
@@ -373,7 +347,7 @@ struct E4m3Rows {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const u32x4 w = b.v[u >> 1];
-      const bf16x8 v = u & 1 ? to_bf16(w.z, w.w) : to_bf16(w.x, w.y);
+      const bf16x8 v = u & 1 ? to_bf16(w.z, w.w, 1.f) : to_bf16(w.x, w.y, 1.f);
       st.acc[u] *= alpha;
       st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_hi, st.acc[u], 0, 0, 0);
       st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p_lo, st.acc[u], 0, 0, 0);
@@ -394,11 +368,11 @@ struct E4m3Rows {
 // W wavefronts (four) per workgroup, two register buffers of a block each (three and
 // four, and eight or twelve wavefronts, measured no faster), within 168 registers for
 // e4m3 rows, so that three workgroups fit a CU.  Bound by HBM where the rows are many:
-// 256 heads of 9,216 e4m3 rows 95 to 100 us (6.1 to 6.4 TB/s; 117 with the keys converted
-// to bf16 and the values one at a time), of 8,250 in a decode window 90 us, where the
-// bf16 launch takes 174; 256 heads attending to 38 of 288 bf16 blocks 28 us (5.7 TB/s) and 8
-// us for the choice.  Bound by latency where they are few: 8 heads of 2,200 rows 10.0 us
-// (slot record, rows, partials out, counter, partials in), two of 200 6.5.
+// 256 heads of 9,216 e4m3 rows 94 to 99 us (6.2 to 6.5 TB/s), of 8,250 in a decode window
+// 88 us, where the bf16 launch takes 167; 256 heads attending to 38 of 288 bf16 blocks 28 us
+// (5.7 TB/s) and 8 us for the choice.  Bound by latency where they are few: 8 heads of
+// 2,200 rows 9.3 us (slot record, rows, partials out, counter, partials in), two of 200
+// 5.7.
 template <typename R, int W, int MINW, bool PAGED, bool LIST>
 __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
     AttnLaunch a, BlockChoice ch, SlotOrder order, Paging pg, uint8_t* k_scale, uint8_t* v_scale,

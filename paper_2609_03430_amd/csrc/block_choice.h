@@ -12,9 +12,9 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // Candidates of a head that its attention's workgroups choose from themselves, each
 // all of them: a launch of its own for the choice costs more than scoring the head
-// once per split (microseconds per step, here and by a launch: one request of 9,000
-// rows 17.7 and 20.6, of 16,000 20.3 and 21.0, 8 of 16,000 28 and 30, 32 of 16,000 45 and
-// 52; but one of 24,000 26 and 21.5, 32 of 24,000 59 and 55).
+// once per split (bf16 rows, microseconds per layer, here and by a launch: one request
+// of 9,000 rows 17.7 and 20.5, of 16,000 20.5 and 20.9, 8 of 16,000 28 and 31, 32 of
+// 16,000 44 and 52; but one of 24,000 25 and 21, where 32 of 24,000 take 50 and 52 to 55).
 constexpr int kFusedBlocks = 512;
 
 constexpr float kMaxBf16 = 3.3895313892515355e38f;

@@ -116,8 +116,8 @@ struct ra_cache {
   // Brings `order` up to date, at the first launch of a step that asks for it (not
   // the first layer: launches that take no order may come before), and returns it where
   // the caches are ragged: heads that start last should be short (microseconds per step,
-  // slots as they come and the longest first: 1,280 heads of 1,000 to 9,000 e4m3 rows 340
-  // and 289, 480 paged ones of 300 to 4,100 76 and 68).  Lengths hardly change their
+  // slots as they come and the longest first: 1,280 heads of 1,000 to 9,000 e4m3 rows 338
+  // and 299, 480 paged ones of 300 to 4,100 76 and 68).  Lengths hardly change their
   // order between steps, so an insertion sort goes over them once.
   const ra::SlotOrder* refresh_order() {
     if (n_appended == 0 || order_stale || !order_sorted) {
