@@ -74,6 +74,12 @@ struct Pools {
   const uint8_t* v_scale;
 };
 
+// What this wavefront's lanes have written to LDS is there for its other lanes.
+__device__ __forceinline__ void staged_in_wave() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // 2^x, a result below 2^-126 flushed to zero: nothing beside a weight of 1.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -101,13 +107,13 @@ struct Bf16Rows {
                static_cast<const uint16_t*>(p.v) + row * kHeadDim, 0, lm);
   }
   // The step's pair, as bf16 in LDS: a lane's two channels of each (called by one whole
-  // wavefront).
+  // wavefront, which reads the other lanes' once they are staged_in_wave).
   struct New {
     uint16_t k[kHeadDim], v[kHeadDim];
     __device__ __forceinline__ void stage(uint32_t wk, uint32_t wv) {
       const int lane = threadIdx.x & 63;
-      reinterpret_cast<uint32_t*>(k)[lane] = wk;
-      reinterpret_cast<uint32_t*>(v)[lane] = wv;
+      __builtin_memcpy(k + 2 * lane, &wk, 4);
+      __builtin_memcpy(v + 2 * lane, &wv, 4);
     }
     // .. at row `at` of the block, zeros above it
     __device__ __forceinline__ void patch(Block& b, int at, const LaneMap& lm) const {
@@ -222,12 +228,12 @@ struct E4m3Rows {
       const uint32_t bk = e4m3_scale_byte(max_over_groups(max_over_row16(mk)));
       const uint32_t bv = e4m3_scale_byte(max_over_groups(max_over_row16(mv)));
       const float ik = e4m3_inverse(bk), iv = e4m3_inverse(bv);
-      reinterpret_cast<uint16_t*>(k)[lane] =
-          static_cast<uint16_t>(e4m3_pack2<false>(e4m3_clamp(bf16_low(wk) * ik, bk),
-                                                  e4m3_clamp(bf16_high(wk) * ik, bk), 0u));
-      reinterpret_cast<uint16_t*>(v)[lane] =
-          static_cast<uint16_t>(e4m3_pack2<false>(e4m3_clamp(bf16_low(wv) * iv, bv),
-                                                  e4m3_clamp(bf16_high(wv) * iv, bv), 0u));
+      const uint32_t ck = e4m3_pack2<false>(e4m3_clamp(bf16_low(wk) * ik, bk),
+                                            e4m3_clamp(bf16_high(wk) * ik, bk), 0u);
+      const uint32_t cv = e4m3_pack2<false>(e4m3_clamp(bf16_low(wv) * iv, bv),
+                                            e4m3_clamp(bf16_high(wv) * iv, bv), 0u);
+      __builtin_memcpy(k + 2 * lane, &ck, 2);
+      __builtin_memcpy(v + 2 * lane, &cv, 2);
       if (lane == 0) {
         ks = bk;
         vs = bv;
@@ -265,8 +271,9 @@ struct E4m3Rows {
       const int lane = threadIdx.x & 63;
       uint8_t* kp = static_cast<uint8_t*>(a.kpool);
       uint8_t* vp = static_cast<uint8_t*>(a.vpool);
-      reinterpret_cast<uint16_t*>(kp + row * kHeadDim)[lane] =
-          reinterpret_cast<const uint16_t*>(k)[lane];
+      uint16_t two;
+      __builtin_memcpy(&two, k + 2 * lane, 2);
+      __builtin_memcpy(kp + row * kHeadDim + 2 * lane, &two, 2);
       for (int c = lane; c < kHeadDim; c += 64)
         vp[(row & ~int64_t(7)) * kHeadDim + c * 8 + (row & 7)] = v[c];
       if (lane == 0) {
@@ -465,7 +472,10 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_blocks_kernel(
     load(x1, min(b0 + 1, last));
     typename R::Query q;
     q.set(raw, qi < G);
-    if (owns_last) s_new.stage(new_k, new_v);
+    if (owns_last) {
+      s_new.stage(new_k, new_v);
+      staged_in_wave();
+    }
     // two register buffers in turn; every prefetch is issued (the last block's again
     // once there is none left), so that the wait for a block leaves the next one's
     // loads in flight
