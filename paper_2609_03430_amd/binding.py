@@ -219,6 +219,12 @@ def _stream(stream):
     return int(stream)
 
 
+def _torch_stream(handle, device):
+    """The torch stream of a raw handle."""
+    return (torch.cuda.ExternalStream(handle, device) if handle
+            else torch.cuda.default_stream(device))
+
+
 def make_config(num_layers, num_q_heads, num_kv_heads, budget_k, recent_r=64,
                 evict_every=64, budget_mode=RA_BUDGET_EVICTABLE, dtype=RA_BF16,
                 max_seqs=1, head_dim=128, attn_split=0,
@@ -541,6 +547,7 @@ class Cache:
         self.workspace = torch.empty(ra_workspace_bytes(cfg), dtype=torch.uint8,
                                      device=self.device)
         self.bounds = self.sparse_workspace = None       # (attach_sparse)
+        self._sparse_streams = set()                     # handles they were used on
         self.handle = ra_cache_create(cfg, self.k_pool, self.v_pool, self.pos_pool,
                                       pool_rows, self.meta, stream)
 
@@ -564,16 +571,27 @@ class Cache:
 
     def attach_sparse(self, n_blocks, stream=None):
         """Bounds and workspace for sparse steps of up to n_blocks blocks per head (the
-        bounds attached before are computed anew)."""
+        bounds attached before are computed anew).  They are allocated for `stream`, and
+        their memory is kept until the sparse steps made of them have ended, whatever
+        streams these ran on."""
         size = ra_sparse_bytes(self.cfg, self.pool_rows)
         if size == 0:
             raise RandAttnError(RA_ERR_UNSUPPORTED, "ra_sparse_bytes")
-        bounds = torch.empty(size, dtype=torch.uint8, device=self.device)
-        workspace = torch.empty(ra_sparse_workspace_bytes(self.cfg, n_blocks), dtype=torch.uint8,
-                                device=self.device)
-        ra_sparse_attach(self.handle, bounds, stream)
+        handle = _stream(stream)
+        with torch.cuda.stream(_torch_stream(handle, self.device)):
+            bounds = torch.empty(size, dtype=torch.uint8, device=self.device)
+            workspace = torch.empty(ra_sparse_workspace_bytes(self.cfg, n_blocks),
+                                    dtype=torch.uint8, device=self.device)
+        ra_sparse_attach(self.handle, bounds, handle)
         self.bounds, self.sparse_workspace = bounds, workspace
+        self._sparse_streams = set()
 
     def decode_sparse(self, layer, n_blocks, recent_rows, q, k_new, v_new, out, stream=None):
+        handle = _stream(stream)
+        if handle not in self._sparse_streams and self.bounds is not None:
+            used_on = _torch_stream(handle, self.device)
+            self.bounds.record_stream(used_on)
+            self.sparse_workspace.record_stream(used_on)
+            self._sparse_streams.add(handle)
         ra_sparse_attention(self.handle, layer, n_blocks, recent_rows, q, k_new, v_new, out,
-                            self.sparse_workspace, stream)
+                            self.sparse_workspace, handle)
