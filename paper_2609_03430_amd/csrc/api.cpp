@@ -288,6 +288,12 @@ int mid_plan(const ra_cache* c, Plan& p, int heads, int keys_max, int64_t keys_m
 //     of 9,000 keys, 264 heads 1: 161, 2: 142, 3: 135, 6: 131; 320 1: 166, 2: 152, 3: 144;
 //     384 1: 180, 2: 166, 3: 174; 512 1: 209, 2: 217; 640 1: 280, 2: 268; of 2,200, 264
 //     heads 1: 48, 3: 44; 320 1: 52, 3: 52; 640 1: 87, 2: 94.
+// Steps over chosen blocks, whose splits each repeat the choice, follow the same lines
+// (within 3% of the best at 8 to 256 heads of 9,000 rows, 32 or 128 blocks chosen; these of
+// 32): 8 heads, bf16 1: 23.2, 2: 20.4, 4: 17.8, 8: 17.2, e4m3 1: 19.2, 2: 18.6, 4: 17.2, 8:
+// 16.8; 64 heads 1: 26.3, 2: 24.1, 3: 22.7, 4: 22.5, 8: 24.6 and 1: 22.0, 2: 21.5, 3: 20.7,
+// 8: 23.0; 128 heads 1: 29.3, 2: 29.5, 3: 32.5 and 1: 24.4, 2: 25.4, 3: 26.9; 192 heads 1:
+// 35.6, 2: 40.0 and 1: 29.9, 2: 33.3; 256 heads 1: 40.7, 2: 44.5 and 1: 32.8, 2: 35.0.
 // The partials of heads past 256 must fit the no-alloc entry point's array, which whole
 // heads do not need (one plan serves all entry points).
 Plan ra::host::plan_blocks(const ra_cache* c, int64_t keys_max, int heads) {

@@ -68,8 +68,8 @@ __device__ __forceinline__ void over_groups(i16x2& x, F&& join) {
 // One wavefront per block: lane (c8, r4) folds eight channels of eight rows as packed
 // 16-bit integers, the four row groups join by lane swaps; rows with an infinity or a NaN
 // are folded again without them.  Bound by HBM, the key rows once per row that an event
-// or a write has changed: 256 heads of 9,216 rows 108 us in bf16 (5.6 TB/s), 63 in e4m3
-// (4.8; folded in fp32 with shuffles 71).  Two, four or eight blocks to a wavefront, the
+// or a write has changed: 256 heads of 9,216 rows 108 us in bf16 (5.8 TB/s, the bounds
+// written included), 63 in e4m3 (5.1; folded in fp32 with shuffles 71).  Two, four or eight blocks to a wavefront, the
 // next one's rows prefetched, and for e4m3 16-byte units of four rows, took 5 to 60%
 // longer.  Grid: (ceil(blocks / 4), Hkv, ranges x layers).
 template <bool E4M3, bool PAGED>
