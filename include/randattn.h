@@ -70,7 +70,7 @@ extern "C" {
 typedef enum {
   RA_OK = 0,
   RA_ERR_INVALID_ARG = -1,  /* bad pointer, index, shape or config field */
-  RA_ERR_CAPACITY = -2,     /* pool full, or a head region would overflow */
+  RA_ERR_CAPACITY = -2,     /* pool full, a head region would overflow, or no host memory */
   RA_ERR_BUDGET = -3,       /* TOTAL mode and the prompt exceeds budget_k */
   RA_ERR_UNSUPPORTED = -4,  /* valid but not implemented (head_dim, group) */
   RA_ERR_HIP = -5,          /* a HIP call or kernel launch failed */

@@ -416,10 +416,23 @@ ra_status ra::host::check_decode(const ra_cache* c, int32_t layer, const void* q
 ra_status ra::host::grow_for_step(ra_cache* c, hipStream_t s) {
   if (!c->is_paged()) return RA_OK;
   std::vector<ra::TableEntry> te;
+  int64_t wanted = 0;
+  // room for the new entries first: without it nothing changes
+  try {
+    for (int i = c->slot_lo; i < c->slot_hi; ++i) {
+      if (!c->mirror[i].active) continue;
+      const int64_t n = c->groups_short(i, c->mirror[i].len + 1);
+      if (n > 0) c->groups[i].reserve(c->groups[i].size() + n);
+      wanted += n;
+    }
+    te.reserve(wanted);
+  } catch (const std::bad_alloc&) {
+    return RA_ERR_CAPACITY;
+  }
+  if (wanted == 0) return RA_OK;
   for (int i = c->slot_lo; i < c->slot_hi; ++i)
     if (c->mirror[i].active) c->grow(i, c->mirror[i].len + 1, te);
-  if (!te.empty())
-    RA_LAUNCH(ra::launch_table_set(c->shape(), te.data(), static_cast<int>(te.size()), s));
+  RA_LAUNCH(ra::launch_table_set(c->shape(), te.data(), static_cast<int>(te.size()), s));
   return RA_OK;
 }
 

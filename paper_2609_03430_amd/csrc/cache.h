@@ -52,6 +52,7 @@ Plan plan_blocks(const ra_cache* c, int64_t keys_max, int heads);
 ra_status check_decode(const ra_cache* c, int32_t layer, const void* q, const void* k_new,
                        const void* v_new, const void* out);
 // Paged layout: pages for the rows this step appends (the first layer of the step).
+// RA_ERR_CAPACITY, nothing changed, if the host has no memory for their entries.
 ra_status grow_for_step(ra_cache* c, hipStream_t s);
 // Moves the key/value rows of every sequence whose last event deferred them (their
 // positions are already compacted); a call that reads or writes rows, or plans
