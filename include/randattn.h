@@ -31,7 +31,8 @@
  *   error leaves device state untouched.  A failed launch returns
  *   RA_ERR_HIP (ra_last_hip_error gives the hipError_t); after RA_ERR_HIP
  *   from a call that launches several kernels (ra_seq_begin, a paged or
- *   move-carrying ra_decode_attention, ra_sparse_attention, ra_end_step, ra_evict_now,
+ *   move-carrying ra_decode_attention, ra_sparse_attention, ra_biased_attention,
+ *   ra_end_step, ra_evict_now,
  *   ra_fast_forward, ra_seq_fast_forward, ra_scored_evict) the host mirror
  *   and the device state may disagree, and the cache should be destroyed.
  *   Nothing throws across the ABI.
@@ -456,6 +457,137 @@ ra_status ra_sparse_attention(ra_cache* cache, int32_t layer, int32_t n_blocks,
                               int32_t recent_rows, const void* q, const void* k_new,
                               const void* v_new, void* out, void* workspace,
                               size_t workspace_bytes, void* stream);
+
+/* ---- rotary positions ------------------------------------------------------------ */
+
+/* The first `dims` channels of a row are turned in pairs by the row's position p: pair i of
+ * dims / 2, of channels a and b, by the angle p * f_i,
+ *   a' = m (a cos - b sin),  b' = m (b cos + a sin),  f_i = base^(-2i / dims);
+ * the other channels stay.  Angles are taken in 64 bits, sines, cosines and products in
+ * 32.  For contexts longer than the model's own, f_i is scaled (ra_rotary_scaling) to
+ * f_i (t + (1 - t) / factor) with a share t in [0, 1] of each pair. */
+typedef enum {
+  RA_PAIRS_HALVES = 0,   /* pair i: channels i and i + dims / 2 */
+  RA_PAIRS_ADJACENT = 1  /* pair i: channels 2i and 2i + 1 */
+} ra_rotary_pairs;
+
+typedef enum {
+  RA_ROTARY_PLAIN = 0,      /* t = 1: f_i as it is (factor is not read) */
+  RA_ROTARY_LINEAR = 1,     /* t = 0: every pair slowed by factor */
+  RA_ROTARY_ROTATIONS = 2,  /* t rises from 0 to 1 with the turns that a pair makes over
+                               original_len positions, n = original_len f_i / 2 pi:
+                               t = (n - low) / (high - low) */
+  RA_ROTARY_CHANNELS = 3    /* t falls from 1 to 0 with the pair's index, from i1 =
+                               floor(i(high)) to i0 = ceil(i(low)) (within [0, dims - 1]),
+                               i(n) = dims ln(original_len / 2 pi n) / (2 ln base) being the
+                               pair that makes n turns: t = 1 - (i - i1) / (i0 - i1) */
+} ra_rotary_scaling;
+
+typedef struct {
+  double base;           /* > 1 */
+  double factor;         /* > 0, unless RA_ROTARY_PLAIN */
+  double low, high;      /* ROTATIONS and CHANNELS: 0 < low < high, in turns */
+  double magnitude;      /* m, which the turned channels are multiplied by; 0 counts as 1 */
+  int32_t dims;          /* even, in [2, 128] */
+  int32_t pairs;         /* ra_rotary_pairs */
+  int32_t scaling;       /* ra_rotary_scaling */
+  int32_t original_len;  /* ROTATIONS and CHANNELS: > 0 */
+} ra_rotary;
+
+/* A step's queries and new keys (the arrays of ra_decode_attention) of every active slot,
+ * turned by the position that the step's row will have: prompt_len + step, read from the
+ * slot's record on the device, so a captured call turns by the right position at every
+ * replay.  The step may be open; the cache is not changed.  q or k_new may be NULL.
+ * Outputs may be the inputs themselves (no other overlap); inactive slots' rows are left
+ * as they are. */
+ra_status ra_rotate_step(const ra_cache* cache, const ra_rotary* rotary, const void* q,
+                         const void* k_new, void* q_out, void* k_out, void* stream);
+
+/* Rows x [heads][rows][128] (RA_F32 or RA_BF16), row j of each head at position
+ * first_position + j, or with dev_positions at dev_positions[head][j] (int32, of any sign;
+ * first_position is not read): the prompt's keys before ra_seq_begin, or rows and
+ * positions as ra_export_rows and ra_export_positions give them.  `out` may be x itself
+ * (no other overlap).  Runs on the current device. */
+ra_status ra_rotate_rows(const ra_rotary* rotary, int32_t dtype, const void* x, void* out,
+                         int64_t heads, int32_t rows, int32_t first_position,
+                         const int32_t* dev_positions, void* stream);
+
+/* ---- decode attention under a score rule ------------------------------------------- */
+
+/* What becomes of the score of a cached row at position p_j, for the new row's position
+ * p_new and query head h, in this order:
+ *   s = scale * (q . k)
+ *   s = cap * tanh(s / cap)               with a cap
+ *   s = s - slope_h * (p_new - p_j)       with slopes
+ *   not attended if p_new - p_j >= window and p_j >= prefix, with a window
+ * Positions are the cached ones, so a rule means the same whatever has been evicted.  A
+ * row that is not attended has no part in the output, infinite or NaN as it may be; the
+ * new row always is.  Of a cache whose rows lie in the order of their positions (all but
+ * hole-fill) only the rows that may be within the window or the prefix are read. */
+typedef struct {
+  float scale;              /* finite, >= 0; 0: 1 / sqrt(head_dim) */
+  float cap;                /* finite, >= 0; 0: none */
+  const float* dev_slopes;  /* [num_q_heads], or NULL: none */
+  int32_t window;           /* >= 0; 0: none */
+  int32_t prefix;           /* >= 0: positions that a window never hides */
+} ra_score_rule;
+
+/* ra_decode_attention under a rule: the same append, arrays, dtypes, layouts, step protocol
+ * and errors, one call per layer and step in its place (the layers of a step may mix both,
+ * with different rules; graph mode and capture as there, dev_slopes being read at each
+ * replay).  A rule of zeros gives ra_decode_attention's result up to rounding.  Row moves
+ * that an event has deferred run first, and events at the end of such steps defer none.
+ * workspace: ra_workspace_bytes, or with weights attached ra_weights_workspace_bytes. */
+ra_status ra_biased_attention(ra_cache* cache, int32_t layer, const ra_score_rule* rule,
+                              const void* q, const void* k_new, const void* v_new, void* out,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- eviction by accumulated attention weight --------------------------------------- */
+
+/* With a weights buffer attached, every cached row of every head has a weight (fp32):
+ *   - a prompt's rows start at 0, as do rows of a fast forward;
+ *   - ra_biased_attention adds to each row the sum of the softmax weights that the group's
+ *     G query heads attend to it with, and sets the new row's to its own sum (rows that a
+ *     window hides gain nothing); the sums are made in a fixed order, so they are the same
+ *     on every run;
+ *   - events (at the end of a step, ra_evict_now, in a fast forward) drop the m candidates of
+ *     least weight, the earliest first among equal ones, in place of the policy's draw (-0
+ *     counts as 0, a NaN as less than any number), and compact the weights with the rows.
+ * Which rows are candidates, how many are dropped and when is as without it.  Every layer's
+ * steps are then made with ra_biased_attention: ra_decode_attention, its _noalloc form,
+ * ra_sparse_attention and ra_scored_evict return RA_ERR_STATE.  Events defer no row moves.
+ * Not with RA_LAYOUT_HOLE_FILL (RA_ERR_UNSUPPORTED).
+ * A preempted request resumes with ra_seq_begin and ra_seq_fast_forward by the steps it had
+ * made (which give it its length and event count), then ra_write_positions, ra_write_rows
+ * and ra_write_weights with what was saved. */
+
+/* Bytes of the weights buffer for a pool of pool_rows rows (4 per row); 0 on a bad config or
+ * one whose layout has no weights. */
+size_t ra_weights_bytes(const ra_config* cfg, int64_t pool_rows);
+
+/* Bytes of ra_biased_attention's workspace with weights attached, for prompts of up to
+ * max_prompt_len rows (the paged layout: the config's max_prompt_len): the split partials and
+ * num_q_heads floats per row.  0 as above, or if such a prompt does not fit the budget. */
+size_t ra_weights_workspace_bytes(const ra_config* cfg, int32_t max_prompt_len);
+
+/* Attach a weights buffer (ra_weights_bytes bytes, 16-byte aligned; contents need not be
+ * set), or detach with NULL.  It is the caller's: zeroing it between steps, in stream order,
+ * starts every request's sums anew.  RA_ERR_STATE with an active sequence or in graph mode. */
+ra_status ra_weights_attach(ra_cache* cache, float* dev_weights, size_t weights_bytes);
+
+/* Slot `seq`'s weights from or to device memory, [L][Hkv][len] (row j belongs to the j-th
+ * cached position).  RA_ERR_STATE without weights attached, in graph mode, inside an open
+ * step or for an inactive slot; ra_export_weights: RA_ERR_CAPACITY, nothing copied, if
+ * out_elems is smaller.  NULL allowed when len is 0. */
+ra_status ra_write_weights(ra_cache* cache, int32_t seq, const float* dev_weights, void* stream);
+ra_status ra_export_weights(ra_cache* cache, int32_t seq, float* dev_out, int64_t out_elems,
+                            void* stream);
+
+/* Overwrite slot `seq`'s cached positions, [L][Hkv][len] int32, ascending and distinct in each
+ * head, the prompt's 0..lp-1 first and all below prompt_len + step: what ra_export_positions
+ * gave for a request that resumes.  Errors as ra_write_weights. */
+ra_status ra_write_positions(ra_cache* cache, int32_t seq, const int32_t* dev_positions,
+                             void* stream);
 
 /* ---- state transfer and audit --------------------------------------------- */
 

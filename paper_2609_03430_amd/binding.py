@@ -33,6 +33,8 @@ RA_LAYOUT_CHRONOLOGICAL, RA_LAYOUT_HOLE_FILL, RA_LAYOUT_PAGED = 0, 1, 2
 RA_POLICY_RANDOM, RA_POLICY_SHARED, RA_POLICY_BLOCK, RA_POLICY_RECENCY = 0, 1, 2, 3
 RA_POLICY_EXTERNAL = 4
 RA_SCORER_SNAPKV, RA_SCORER_RKV, RA_SCORER_VASE = 0, 1, 2
+RA_PAIRS_HALVES, RA_PAIRS_ADJACENT = 0, 1
+RA_ROTARY_PLAIN, RA_ROTARY_LINEAR, RA_ROTARY_ROTATIONS, RA_ROTARY_CHANNELS = 0, 1, 2, 3
 RA_NOALLOC_SCRATCH_BYTES = 8 << 20
 
 # Every entry point declared in include/randattn.h.
@@ -48,7 +50,9 @@ EXPORTS = (
     "ra_last_hip_error", "ra_attention_plan", "ra_window_select",
     "ra_scored_scratch_bytes", "ra_scored_evict",
     "ra_export_rows", "ra_sparse_bytes", "ra_sparse_workspace_bytes", "ra_sparse_attach",
-    "ra_sparse_attention",
+    "ra_sparse_attention", "ra_rotate_step", "ra_rotate_rows", "ra_biased_attention",
+    "ra_weights_bytes", "ra_weights_workspace_bytes", "ra_weights_attach", "ra_write_weights",
+    "ra_export_weights", "ra_write_positions",
 )
 
 
@@ -79,6 +83,31 @@ def make_scorer(scorer, rkv_lambda=0.1, rkv_threshold=0.9, rkv_recent_dups=1,
                 vase_n_large=-1, vase_seed=0):
     return ra_scorer_params(scorer, rkv_lambda, rkv_threshold, rkv_recent_dups,
                             vase_n_large, vase_seed)
+
+
+class ra_rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("base", "factor", "low", "high", "magnitude")] + \
+        [(n, ctypes.c_int32) for n in ("dims", "pairs", "scaling", "original_len")]
+
+
+def make_rotary(base, dims=128, pairs=RA_PAIRS_HALVES, scaling=RA_ROTARY_PLAIN, factor=1.0,
+                low=1.0, high=4.0, original_len=8192, magnitude=1.0):
+    """factor, low, high and original_len apply to the scalings that read them."""
+    return ra_rotary(base, factor, low, high, magnitude, dims, pairs, scaling, original_len)
+
+
+class ra_score_rule(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("dev_slopes", ctypes.c_void_p), ("window", ctypes.c_int32),
+                ("prefix", ctypes.c_int32)]
+
+
+def make_score_rule(scale=0.0, cap=0.0, slopes=None, window=0, prefix=0):
+    """slopes: fp32 device tensor of a slope per query head, kept alive by the rule."""
+    _arg(slopes, "make_score_rule", "slopes", torch.float32)
+    rule = ra_score_rule(scale, cap, _ptr(slopes), window, prefix)
+    rule.slopes = slopes
+    return rule
 
 
 class ra_seq_info(ctypes.Structure):
@@ -134,6 +163,15 @@ _SIGS = {
     "ra_sparse_workspace_bytes": (_SZ, [_CFG, _I32]),
     "ra_sparse_attach": (_I32, [_P, _P, _SZ, _P]),
     "ra_sparse_attention": (_I32, [_P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _SZ, _P]),
+    "ra_rotate_step": (_I32, [_P, _P, _P, _P, _P, _P, _P]),
+    "ra_rotate_rows": (_I32, [_P, _I32, _P, _P, _I64, _I32, _I32, _P, _P]),
+    "ra_biased_attention": (_I32, [_P, _I32, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "ra_weights_bytes": (_SZ, [_CFG, _I64]),
+    "ra_weights_workspace_bytes": (_SZ, [_CFG, _I32]),
+    "ra_weights_attach": (_I32, [_P, _P, _SZ]),
+    "ra_write_weights": (_I32, [_P, _I32, _P, _P]),
+    "ra_export_weights": (_I32, [_P, _I32, _P, _I64, _P]),
+    "ra_write_positions": (_I32, [_P, _I32, _P, _P]),
 }
 
 _handle = None
@@ -511,6 +549,99 @@ def ra_sparse_attention(handle, layer, n_blocks, recent_rows, q, k_new, v_new, o
                                       _stream(stream)), "ra_sparse_attention")
 
 
+def _step_array(handle, where, name, x, out, heads_of):
+    """Checks one of a step's arrays and the one it is turned into."""
+    cfg = _cfg_of(handle)
+    if cfg is None:
+        return
+    n = cfg.max_seqs * heads_of(cfg) * cfg.head_dim
+    _arg(x, where, name, _cache_dtype(cfg), n)
+    _arg(out, where, name + "_out", _cache_dtype(cfg), n)
+
+
+def ra_rotate_step(handle, rotary, q, k_new, q_out, k_out, stream=None):
+    where = "ra_rotate_step"
+    _step_array(handle, where, "q", q, q_out, lambda cfg: cfg.num_q_heads)
+    _step_array(handle, where, "k_new", k_new, k_out, lambda cfg: cfg.num_kv_heads)
+    _check(_lib().ra_rotate_step(handle, ctypes.byref(rotary), _ptr(q), _ptr(k_new), _ptr(q_out),
+                                 _ptr(k_out), _stream(stream)), where)
+
+
+def ra_rotate_rows(rotary, x, out, first=0, positions=None, stream=None):
+    """Rows x [..., rows, 128] (fp32 or bf16) into `out`, which may be x; positions: int32,
+    one per row of x."""
+    where = "ra_rotate_rows"
+    _arg(x, where, "x")
+    if x.dtype not in (torch.float32, torch.bfloat16) or x.dim() < 2 or x.shape[-1] != 128:
+        raise RandAttnError(RA_ERR_INVALID_ARG, where + " (x: not fp32 or bf16 rows of 128)")
+    rows = x.shape[-2]
+    n = x.numel() // 128
+    _arg(out, where, "out", x.dtype, x.numel())
+    _arg(positions, where, "positions", torch.int32, n)
+    if any(t is not None and t.device != x.device for t in (out, positions)):
+        raise RandAttnError(RA_ERR_INVALID_ARG, where + " (arrays on different devices)")
+    with torch.cuda.device(x.device):
+        _check(_lib().ra_rotate_rows(ctypes.byref(rotary),
+                                     RA_F32 if x.dtype == torch.float32 else RA_BF16, _ptr(x),
+                                     _ptr(out), n // rows if rows else 0, rows, int(first),
+                                     _ptr(positions), _stream(stream)), where)
+
+
+def ra_biased_attention(handle, layer, rule, q, k_new, v_new, out, workspace, stream=None):
+    where = "ra_biased_attention"
+    _decode_args(handle, where, q, k_new, v_new, out)
+    cfg, slopes = _cfg_of(handle), getattr(rule, "slopes", None)
+    if cfg is not None:
+        _arg(slopes, where, "slopes", torch.float32, cfg.num_q_heads)
+    _arg(workspace, where, "workspace")
+    _check(_lib().ra_biased_attention(handle, int(layer), ctypes.byref(rule), _ptr(q), _ptr(k_new),
+                                      _ptr(v_new), _ptr(out), _ptr(workspace),
+                                      0 if workspace is None else _bytes(workspace),
+                                      _stream(stream)), where)
+
+
+def ra_weights_bytes(cfg, pool_rows):
+    return int(_lib().ra_weights_bytes(ctypes.byref(cfg), int(pool_rows)))
+
+
+def ra_weights_workspace_bytes(cfg, max_prompt_len):
+    return int(_lib().ra_weights_workspace_bytes(ctypes.byref(cfg), int(max_prompt_len)))
+
+
+def ra_weights_attach(handle, weights):
+    """Attach a weights buffer (an fp32 device tensor kept alive by the caller), or detach
+    with None."""
+    _arg(weights, "ra_weights_attach", "weights", torch.float32)
+    _check(_lib().ra_weights_attach(handle, _ptr(weights),
+                                    0 if weights is None else _bytes(weights)),
+           "ra_weights_attach")
+
+
+def _row_values(handle, seq):
+    """Elements of an array of one value per cached row of slot `seq`."""
+    cfg = _cfg_of(handle)
+    return 0 if cfg is None else _rows_needed(handle, seq, False)[1] // cfg.head_dim
+
+
+def ra_write_weights(handle, seq, weights, stream=None):
+    where = "ra_write_weights"
+    _arg(weights, where, "weights", torch.float32, _row_values(handle, seq))
+    _check(_lib().ra_write_weights(handle, int(seq), _ptr(weights), _stream(stream)), where)
+
+
+def ra_export_weights(handle, seq, out, stream=None):
+    where = "ra_export_weights"
+    _arg(out, where, "out", torch.float32)
+    _check(_lib().ra_export_weights(handle, int(seq), _ptr(out), 0 if out is None else out.numel(),
+                                    _stream(stream)), where)
+
+
+def ra_write_positions(handle, seq, positions, stream=None):
+    where = "ra_write_positions"
+    _arg(positions, where, "positions", torch.int32, _row_values(handle, seq))
+    _check(_lib().ra_write_positions(handle, int(seq), _ptr(positions), _stream(stream)), where)
+
+
 def ra_attention_plan(handle):
     """(split_keys, max_splits, waves) of the next attention launch."""
     sk, ms, w = ctypes.c_int32(0), ctypes.c_int32(0), ctypes.c_int32(0)
@@ -548,6 +679,8 @@ class Cache:
                                      device=self.device)
         self.bounds = self.sparse_workspace = None       # (attach_sparse)
         self._sparse_streams = set()                     # handles they were used on
+        self.weights = self.weights_workspace = None     # (attach_weights)
+        self._weight_streams = set()
         self.handle = ra_cache_create(cfg, self.k_pool, self.v_pool, self.pos_pool,
                                       pool_rows, self.meta, stream)
 
@@ -595,3 +728,32 @@ class Cache:
             self._sparse_streams.add(handle)
         ra_sparse_attention(self.handle, layer, n_blocks, recent_rows, q, k_new, v_new, out,
                             self.sparse_workspace, handle)
+
+    def attach_weights(self, max_prompt_len, stream=None):
+        """Accumulated weights, and the workspace of the steps that add to them, for prompts
+        of up to max_prompt_len rows.  They are allocated for `stream`, and their memory is
+        kept until the steps made with them have ended, whatever streams these ran on."""
+        size = ra_weights_bytes(self.cfg, self.pool_rows)
+        if size == 0:
+            raise RandAttnError(RA_ERR_UNSUPPORTED, "ra_weights_bytes")
+        work = ra_weights_workspace_bytes(self.cfg, max_prompt_len)
+        if work == 0:
+            raise RandAttnError(RA_ERR_INVALID_ARG, "ra_weights_workspace_bytes")
+        with torch.cuda.stream(_torch_stream(_stream(stream), self.device)):
+            weights = torch.zeros(size // 4, dtype=torch.float32, device=self.device)
+            workspace = torch.empty(work, dtype=torch.uint8, device=self.device)
+        ra_weights_attach(self.handle, weights)
+        self.weights, self.weights_workspace = weights, workspace
+        self._weight_streams = set()
+
+    def decode_biased(self, layer, rule, q, k_new, v_new, out, stream=None):
+        workspace = self.workspace
+        if self.weights is not None:
+            handle = _stream(stream)
+            workspace = self.weights_workspace
+            if handle not in self._weight_streams:
+                used_on = _torch_stream(handle, self.device)
+                self.weights.record_stream(used_on)
+                workspace.record_stream(used_on)
+                self._weight_streams.add(handle)
+        ra_biased_attention(self.handle, layer, rule, q, k_new, v_new, out, workspace, stream)

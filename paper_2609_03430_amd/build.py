@@ -20,8 +20,9 @@ LIB = os.path.join(LIBDIR, "librandattn.so")
 OBJDIR = os.path.join(ROOT, "_build")
 # per-kernel register, scratch and LDS use reported by the compiler
 RESOURCES = os.path.join(OBJDIR, "kernel_resources.json")
-SOURCES = ["attention.hip", "attn_blocks.hip", "blocks.hip", "evict.hip", "state.hip",
-           "window_score.hip", "scored.hip", "api.cpp", "api_blocks.cpp"]
+SOURCES = ["attention.hip", "attn_blocks.hip", "attn_biased.hip", "blocks.hip", "evict.hip",
+           "weights.hip", "rotary.hip", "state.hip", "window_score.hip", "scored.hip", "api.cpp",
+           "api_blocks.cpp", "api_biased.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -460,6 +460,12 @@ hipError_t launch_event(ra_cache* c, int lo, int hi, int candidates, bool deferr
                         const ra::DueList& list, hipStream_t s) {
   ra::Shape sh = c->shape();
   int32_t* drops = deferred ? c->drops : nullptr;
+  const auto evict = [&](int a, int b) {
+    return c->weights ? c->weight_hooks->event(sh, c->meta, c->kpool, c->vpool, c->pos, c->weights,
+                                               a, b, candidates, false, s)
+                      : ra::launch_evict(sh, c->meta, c->kpool, c->vpool, c->pos, a, b, candidates,
+                                         deferred, s, drops, c->cfg.evict_every);
+  };
   const int64_t heads = static_cast<int64_t>(c->cfg.num_layers) * c->cfg.num_kv_heads;
   if (list.n && list.n * heads <= kMaxHeadsPerLaunch) {
     sh.due = &list;
@@ -471,13 +477,9 @@ hipError_t launch_event(ra_cache* c, int lo, int hi, int candidates, bool deferr
         if (c->mirror[i].active) rows += c->mirror[i].len;
       sh.cached = rows * heads * 2 * ra::kHeadDim * static_cast<int64_t>(c->elem) <= kCachedBytes;
     }
-    return ra::launch_evict(sh, c->meta, c->kpool, c->vpool, c->pos, list.slot[0],
-                            list.slot[0] + 1, candidates, deferred, s, drops, c->cfg.evict_every);
+    return evict(list.slot[0], list.slot[0] + 1);
   }
-  return by_slot_chunks(c->cfg, lo, hi, [&](int a, int b) {
-    return ra::launch_evict(sh, c->meta, c->kpool, c->vpool, c->pos, a, b, candidates, deferred,
-                            s, drops, c->cfg.evict_every);
-  });
+  return by_slot_chunks(c->cfg, lo, hi, evict);
 }
 
 // Marks the layer appended and launches its append + attention with the
@@ -502,6 +504,7 @@ ra_status launch_decode(ra_cache* c, int32_t layer, const void* q, const void* k
   }
   c->appended[layer] = 1;
   ++c->n_appended;
+  c->biased_step = false;
   if (c->slot_hi <= c->slot_lo) return RA_OK;
   ra::AttnLaunch a{};
   a.meta = c->meta;
@@ -791,6 +794,8 @@ ra_status ra_seq_begin(ra_cache* c, int32_t seq, int32_t prompt_len, uint64_t se
     if (e == hipSuccess)
       e = ra::launch_write_rows(c->shape(), M, seq, prompt_len, dev_k_prompt, dev_v_prompt,
                                 nullptr, c->kpool, c->vpool, c->pos, s);
+    if (e == hipSuccess && c->weights)
+      e = c->weight_hooks->set(c->shape(), M, seq, 0, prompt_len, nullptr, c->weights, s);
     if (e == hipSuccess) e = ra::launch_seq_set(c->meta, seq, M, s);
     if (e != hipSuccess) {   // the slot stays inactive: its pages go back
       c->shrink(seq, 0);
@@ -821,6 +826,8 @@ ra_status ra_seq_begin(ra_cache* c, int32_t seq, int32_t prompt_len, uint64_t se
   // leaves the slot inactive on the device as in the mirror
   RA_LAUNCH(ra::launch_write_rows(c->shape(), M, seq, prompt_len, dev_k_prompt,
                                   dev_v_prompt, nullptr, c->kpool, c->vpool, c->pos, s));
+  if (c->weights)
+    RA_LAUNCH(c->weight_hooks->set(c->shape(), M, seq, 0, prompt_len, nullptr, c->weights, s));
   RA_LAUNCH(ra::launch_seq_set(c->meta, seq, M, s));
   const int64_t rest = it->second - need;
   c->free_rows.erase(it);
@@ -873,6 +880,7 @@ ra_status ra_decode_attention(ra_cache* c, int32_t layer, const void* q,
                               void* stream) {
   const ra_status st = check_decode(c, layer, q, k_new, v_new, out);
   if (st != RA_OK) return st;
+  if (c->weights) return RA_ERR_STATE;   // (the new rows would have none)
   if (!workspace || workspace_bytes < ra_workspace_bytes(&c->cfg)) return RA_ERR_INVALID_ARG;
   const size_t items = static_cast<size_t>(c->cfg.max_seqs) * c->cfg.num_kv_heads * ra::kMaxSplits;
   float* ws = static_cast<float*>(workspace);
@@ -886,6 +894,7 @@ ra_status ra_decode_attention_noalloc(ra_cache* c, int32_t layer, const void* q,
                                       void* stream) {
   const ra_status st = check_decode(c, layer, q, k_new, v_new, out);
   if (st != RA_OK) return st;
+  if (c->weights) return RA_ERR_STATE;   // (the new rows would have none)
   if (!c->scratch) return RA_ERR_STATE;
   // partial slots only for the splits this launch has, packed per head; the
   // limit counts plan.partials of them, never fewer than the launch uses
@@ -923,8 +932,11 @@ ra_status ra_end_step(ra_cache* c, void* stream, int32_t* n_evicted) {
     // every head's workgroup reads on the device whether its sequence is
     // due; the mirror stays that of the entry into graph mode
     RA_LAUNCH(by_slot_chunks(c->cfg, c->slot_lo, c->slot_hi, [&](int lo, int hi) {
-      return ra::launch_evict(c->shape(), c->meta, c->kpool, c->vpool, c->pos, lo, hi,
-                              c->graph_candidates, false, s);
+      return c->weights
+                 ? c->weight_hooks->event(c->shape(), c->meta, c->kpool, c->vpool, c->pos,
+                                          c->weights, lo, hi, c->graph_candidates, false, s)
+                 : ra::launch_evict(c->shape(), c->meta, c->kpool, c->vpool, c->pos, lo, hi,
+                                    c->graph_candidates, false, s);
     }));
     return RA_OK;
   }
@@ -951,8 +963,9 @@ ra_status ra_end_step(ra_cache* c, void* stream, int32_t* n_evicted) {
     // that steps of heads with nothing to move run the streaming kernel.
     int n_active = 0;
     for (int i = c->slot_lo; i < c->slot_hi; ++i) n_active += c->mirror[i].active;
-    // (with block bounds attached a step may read part of the rows only: it moves none)
-    const bool defer = c->drops && !c->bounds && due == n_active && attention_plan(c).whole;
+    // (with block bounds attached a step may read part of the rows only: it moves none,
+    // nor do steps of ra_biased_attention, the last of which expects the next one)
+    const bool defer = c->drops && !c->bounds && !c->weights && !c->biased_step && due == n_active && attention_plan(c).whole;
     const int candidates = c->max_candidates_due();
     ra::DueList list;
     if (due <= ra::kDueList) {
@@ -1054,7 +1067,8 @@ namespace {
 // shrink returns and a growth takes again in the same order, so that its table
 // holds throughout.
 bool fast_forward_fused(const ra_cache* c, int lo, int hi, int events, int64_t rows) {
-  if (events == 0 || c->cfg.layout == RA_LAYOUT_HOLE_FILL || rows > ra::kMaxFastForwardRows)
+  if (events == 0 || c->cfg.layout == RA_LAYOUT_HOLE_FILL || rows > ra::kMaxFastForwardRows ||
+      c->weights)
     return false;
   int n_active = 0;
   for (int i = lo; i < hi; ++i) n_active += c->mirror[i].active ? 1 : 0;
@@ -1151,6 +1165,12 @@ ra_status fast_forward_range(ra_cache* c, int lo, int hi, int32_t n_steps, hipSt
         RA_LAUNCH(ra::launch_append_positions(c->shape(), c->meta, c->pos, lo, hi, run, s));
         RA_LAUNCH(ra::launch_advance(c->meta, lo, hi, run, c->cfg.recent_r,
                                      trigger_every(c->cfg), s));
+        for (int i = lo; i < hi && c->weights; ++i) {
+          const SeqMeta& M = c->mirror[i];
+          if (M.active)
+            RA_LAUNCH(c->weight_hooks->set(c->shape(), M, i, M.len, M.len + run, nullptr,
+                                           c->weights, s));
+        }
       }
       int due = 0, candidates = 0;
       for (int i = lo; i < hi; ++i) {
@@ -1167,8 +1187,10 @@ ra_status fast_forward_range(ra_cache* c, int lo, int hi, int32_t n_steps, hipSt
       }
       if (due && launch) {
         RA_LAUNCH(by_slot_chunks(c->cfg, lo, hi, [&](int a, int b) {
-          return ra::launch_evict(c->shape(), c->meta, c->kpool, c->vpool, c->pos, a, b,
-                                  candidates, true, s);
+          return c->weights ? c->weight_hooks->event(c->shape(), c->meta, c->kpool, c->vpool,
+                                                     c->pos, c->weights, a, b, candidates, true, s)
+                            : ra::launch_evict(c->shape(), c->meta, c->kpool, c->vpool, c->pos, a,
+                                               b, candidates, true, s);
         }));
       }
       remaining -= run;
@@ -1304,6 +1326,7 @@ ra_status ra_scored_evict(ra_cache* c, int32_t seq_lo, int32_t seq_hi,
        !std::isfinite(prm->rkv_threshold)))
     return RA_ERR_INVALID_ARG;
   if (c->step_open()) return RA_ERR_STATE;
+  if (c->weights) return RA_ERR_STATE;   // (its compaction moves no weights)
   const int r = c->cfg.recent_r, every = c->cfg.evict_every;
   int max_len = 0, max_cap = 0, due = 0;
   for (int s = seq_lo; s < seq_hi; ++s) {

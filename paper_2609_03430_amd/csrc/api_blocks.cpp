@@ -94,6 +94,7 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
   const ra_status st = ra::host::check_decode(c, layer, q, k_new, v_new, out);
   if (st != RA_OK) return st;
   if (!sparse_supported(c->cfg)) return RA_ERR_UNSUPPORTED;
+  if (c->weights) return RA_ERR_STATE;               // (the new rows would have none)
   if (!c->bounds || c->graph) return RA_ERR_STATE;   // (graph mode: bounds follow the mirror)
   if (!workspace || workspace_bytes < ra_sparse_workspace_bytes(&c->cfg, n_blocks) ||
       (reinterpret_cast<uintptr_t>(workspace) & 15u) != 0)
@@ -171,6 +172,7 @@ ra_status ra_sparse_attention(ra_cache* c, int32_t layer, int32_t n_blocks, int3
                                        c->arrivals, candidates, hs));
   c->appended[layer] = 1;
   ++c->n_appended;
+  c->biased_step = false;
   if (n_active == 0) return RA_OK;
   const Plan plan = ra::host::plan_blocks(c, int64_t(most) * ra::kBlockRows,
                                           n_active * c->cfg.num_kv_heads);

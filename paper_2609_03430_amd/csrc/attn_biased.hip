@@ -1,0 +1,324 @@
+// Decode attention whose scores follow a rule (ra_score_rule), and the accumulated weights
+// of the rows it attends to.  The attention is that of attn_blocks.hip, over the blocks
+// that may hold rows within the window:
+//   s = scale q.k;  s = cap tanh(s / cap);  s -= slope * (p_new - p_j);
+//   s = -inf where p_new - p_j >= window and p_j >= prefix
+// with p the cached positions, so the rule means the same before and after evictions.
+// A weight p_hj = exp(s_hj - m_h) / l_h needs the head's maximum and sum, which are known
+// after its last row: the attention stores the scores (G floats per row, 20 bytes beside
+// the 512 of a bf16 row at G = 5) and add_weights_kernel adds up the weights from them.
+#include "attn_rows.h"
+
+namespace ra {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct BiasedWork : Work {
+  int b0, b1;          // the workgroup's blocks of those attended
+  WindowBlocks win;
+  int now;             // position of the new row
+};
+
+__device__ __forceinline__ BiasedWork locate_biased(const AttnLaunch& a, const BiasLaunch& bias,
+                                                    const SlotOrder& order, int Hkv,
+                                                    const Paging& pg) {
+  BiasedWork w;
+  w.split = blockIdx.x;
+  w.g = blockIdx.y;
+  w.slot = order.n ? order.slot[blockIdx.z] : blockIdx.z;
+  const SeqMeta& M = a.meta[w.slot];
+  w.valid = false;
+  if (!M.active) return w;
+  w.len = M.len;
+  w.n_keys = w.len + 1;
+  w.now = M.prompt_len + M.step;
+  w.win = window_blocks(w.len, bias.ordered ? bias.window : 0, bias.prefix);
+  const int per = a.split_keys / kBlockRows;
+  w.b0 = w.split * per;
+  if (w.b0 >= w.win.n) return w;
+  w.b1 = min(w.b0 + per, w.win.n);
+  w.nsplit = (w.win.n + per - 1) / per;
+  w.rm = row_map(M, w.slot, a.layer * Hkv + w.g, pg);
+  w.valid = true;
+  return w;
+}
+
+// Splits of a head, for the merge.
+struct BiasedSplits {
+  int at, n;
+  __device__ __forceinline__ int slot() const { return at; }
+  __device__ __forceinline__ int operator()(const AttnLaunch&, int) const { return n; }
+};
+
+// Each query's maximum and sum of a head, for add_weights_kernel.
+struct KeepStats {
+  float* to;       // [G][2]
+  __device__ __forceinline__ void operator()(int q, float m, float l) const {
+    to[2 * q] = m;
+    to[2 * q + 1] = l;
+  }
+};
+
+// tanh y, to about an ulp: up to 1 as y less a correction of at most a quarter of it,
+// tanh y = y - y^3 (45045 + 2772 y^2 + 27 y^4) / (135135 + 62370 y^2 + 3150 y^4 + 28 y^6)
+// (the convergent of its continued fraction y / (1 + y^2 / (3 + y^2 / (5 + ..))) that ends
+// with 13), past it as 1 - 2 / (1 + e^2y), where the quotient is a quarter at most.
+__device__ __forceinline__ float tanh_of(float y) {
+  const float a = fabsf(y), y2 = y * y;
+  const float num = 45045.f + y2 * (2772.f + y2 * 27.f);
+  const float den = 135135.f + y2 * (62370.f + y2 * (3150.f + y2 * 28.f));
+  const float near = y - y * y2 * num * __builtin_amdgcn_rcpf(den);
+  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_fast(a * (2.f * kLog2e)));
+  return a > 1.f ? copysignf(far, y) : near;
+}
+
+// The four wavefronts of a workgroup and their register buffers as in attn_blocks_kernel.
+// BYPOS: the rule has slopes or a window, and the positions are read with the rows (e4m3
+// rows then take up to 256 registers, two workgroups to a CU).
+template <typename R, int W, int MINW, bool PAGED, bool BYPOS, bool WEIGH>
+__global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
+    AttnLaunch a, BiasLaunch bias, SlotOrder order, Paging pg, uint8_t* k_scale, uint8_t* v_scale,
+    int G, int Hq, int Hkv) {
+  using E = typename R::Elem;
+  using Two = typename R::New::Two;
+  __shared__ float s_m[W][kMaxGroup];
+  __shared__ float s_l[W][kMaxGroup];
+  __shared__ float s_o[W][kMaxGroup][kHeadDim];
+  __shared__ __align__(16) typename R::New s_new;
+  const BiasedWork w = locate_biased(a, bias, order, Hkv, pg);
+  if (!w.valid) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, qi = lane & 15, grp = lane >> 4;
+  const LaneMap lm = lane_map();
+  const Pools pools{a.kpool, a.vpool, k_scale, v_scale};
+  const int per = (w.b1 - w.b0 + W - 1) / W;
+  const int b0 = __builtin_amdgcn_readfirstlane(w.b0 + wave * per);
+  const int b1 = __builtin_amdgcn_readfirstlane(min(b0 + per, w.b1));
+  const bool has = b0 < b1;
+  const bool owns_last = has && b1 == w.win.n;
+  const float slope = BYPOS && bias.slopes && qi < G ? bias.slopes[w.g * G + qi] * kLog2e : 0.f;
+  const float scale_log2 = bias.scale * kLog2e;
+  const float cap_log2 = bias.cap * kLog2e;
+  const float to_cap = bias.cap > 0.f ? bias.scale / bias.cap : 0.f;
+
+  struct Buffer {
+    typename R::Block rows;
+    int p[BYPOS ? 8 : 1];   // positions of the lane's eight keys
+  };
+  const auto load = [&](Buffer& b, int i) {
+    const int cached = i < w.win.head ? i : i + w.win.shift;
+    const int64_t row = pool_row<PAGED>(w.rm, cached * kBlockRows);
+    R::load(b.rows, pools, row, lm);
+    if constexpr (BYPOS) {
+      const u32x4 lo = ld16(a.pos + row + lm.vrow), hi = ld16(a.pos + row + lm.vrow + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        b.p[e] = static_cast<int>(lo[e]);
+        b.p[4 + e] = static_cast<int>(hi[e]);
+      }
+    }
+  };
+  float* scores = nullptr;
+  if constexpr (WEIGH)
+    scores = bias.scores + (static_cast<int64_t>(w.slot) * Hq + w.g * G + qi) * bias.score_stride +
+             8 * grp;
+
+  Softmax st;
+  st.m = kNoScore;
+  st.l = 0.f;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) st.acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (has) {
+    // the queries and the new pair first: they are made ready while the rows arrive
+    const E* qrow = static_cast<const E*>(a.q) +
+                    (static_cast<int64_t>(w.slot) * Hq + w.g * G + (qi < G ? qi : 0)) * kHeadDim;
+    u32x4 raw[R::Query::kLoads];
+#pragma unroll
+    for (int s = 0; s < R::Query::kLoads; ++s) raw[s] = ld16(qrow + R::Query::channel(s, grp));
+    Two new_k = 0, new_v = 0;
+    if (owns_last) {
+      const int64_t src = (static_cast<int64_t>(w.slot) * Hkv + w.g) * (kHeadDim / 2) + lane;
+      new_k = static_cast<const Two*>(a.k_new)[src];
+      new_v = static_cast<const Two*>(a.v_new)[src];
+    }
+    const int last = b1 - 1;
+    Buffer x0, x1;
+    load(x0, b0);
+    load(x1, min(b0 + 1, last));
+    typename R::Query q;
+    q.set(raw, qi < G);
+    if (owns_last) {
+      s_new.stage(new_k, new_v);
+      staged_in_wave();
+    }
+    // block i; keys from `limit` on are masked out
+    const auto step = [&](Buffer& b, int i, int limit) {
+      float x[8];
+      R::scores(b.rows, q, x);
+      if (bias.cap > 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = cap_log2 * tanh_of(x[e] * to_cap);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= scale_log2;
+      }
+      if constexpr (BYPOS) {
+        uint32_t hidden = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int dist = w.now - b.p[e];
+          x[e] -= slope * static_cast<float>(dist);
+          if (bias.window > 0 && dist >= bias.window && b.p[e] >= bias.prefix) {
+            x[e] = kNegInf;
+            hidden |= 1u << e;
+          }
+        }
+        // a hidden row's value has no part in the products, not even as 0 times it
+        if (__ballot(hidden != 0)) R::hide(b.rows, hidden);
+      }
+      if (limit < 32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * grp + e >= limit) x[e] = kNegInf;
+      }
+      if constexpr (WEIGH) {
+        if (qi < G) {
+          f32x4* to = reinterpret_cast<f32x4*>(scores + static_cast<int64_t>(i) * kBlockRows);
+          to[0] = f32x4{x[0], x[1], x[2], x[3]};
+          to[1] = f32x4{x[4], x[5], x[6], x[7]};
+        }
+      }
+      R::attend(st, b.rows, x);
+    };
+    // two register buffers in turn; every prefetch is issued (the last block's again
+    // once there is none left), so that the wait for a block leaves the next one's
+    // loads in flight
+    int i = b0;
+    for (; i + 1 < last; i += 2) {
+      step(x0, i, 32);
+      load(x0, min(i + 2, last));
+      step(x1, i + 1, 32);
+      load(x1, min(i + 3, last));
+    }
+    if (i < last) {
+      step(x0, i, 32);
+      x0 = x1;
+    }
+    int limit = 32;
+    if (owns_last) {
+      const int at = w.len % kBlockRows;
+      s_new.patch(x0.rows, at, lm);
+      limit = at + 1;
+      if constexpr (BYPOS) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * grp + e >= at) x0.p[e] = w.now;
+      }
+    }
+    step(x0, last, limit);
+    st.l += __shfl_xor(st.l, 16, 64);
+    st.l += __shfl_xor(st.l, 32, 64);
+  }
+  if constexpr (std::is_same_v<R, E4m3Rows>) R::gather_channels(st);
+  const BiasedSplits splits{w.slot, w.nsplit};
+  if constexpr (WEIGH) {
+    const KeepStats keep{bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G)};
+    finish_item<E, W, true, BiasedSplits, typename R::Channels>(
+        a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits, keep);
+  } else {
+    finish_item<E, W, true, BiasedSplits, typename R::Channels>(
+        a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits);
+  }
+  if (owns_last) {
+    const int64_t row = pool_row<PAGED>(w.rm, w.len);
+    s_new.append(a, row, k_scale, v_scale);
+    if (lane == 0) a.pos[row] = w.now;
+  }
+}
+
+// w_j += sum over the group's queries of exp(s_j - m) / l, the new row's weight set.  A
+// row's sum is made by one thread, in the order of the queries: the same on every run.
+// Grid: (runs of 1,024 attended rows, KV heads, slots), four rows to a thread.
+constexpr int kWeighThreads = 256, kWeighRows = 4;
+template <bool PAGED>
+__global__ __launch_bounds__(kWeighThreads) void add_weights_kernel(const SeqMeta* meta, int layer,
+                                                                    BiasLaunch bias, Paging pg,
+                                                                    int G, int Hq, int Hkv) {
+  const int g = blockIdx.y, slot = blockIdx.z;
+  const SeqMeta& M = meta[slot];
+  if (!M.active) return;
+  const int len = M.len;
+  const WindowBlocks win = window_blocks(len, bias.ordered ? bias.window : 0, bias.prefix);
+  const int at = (blockIdx.x * kWeighThreads + threadIdx.x) * kWeighRows;
+  const int i = at / kBlockRows;
+  if (i >= win.n) return;
+  const int j = (i < win.head ? i : i + win.shift) * kBlockRows + at % kBlockRows;
+  if (j > len) return;
+  const int64_t head = static_cast<int64_t>(slot) * Hq + g * G;
+  const float* s = bias.scores + head * bias.score_stride + at;
+  const float* st = bias.stats + 2 * head;
+  const RowMap rm = row_map(M, slot, layer * Hkv + g, pg);
+  f32x4* to = reinterpret_cast<f32x4*>(bias.weights + pool_row<PAGED>(rm, j));
+  f32x4 w = *to, sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int q = 0; q < G; ++q) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(s + q * bias.score_stride);
+    const float m = st[2 * q], inv = 1.f / st[2 * q + 1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += exp2f(x[e] - m) * inv;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = j + e < len ? w[e] + sum[e] : j + e == len ? sum[e] : w[e];
+  *to = w;
+}
+
+template <typename R, bool PAGED, bool BYPOS, bool WEIGH>
+void launch_biased(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hipStream_t s) {
+  constexpr int kMinWaves = BYPOS && R::kWaves > 2 ? 2 : R::kWaves;
+  const SlotOrder order = sh.order ? *sh.order : SlotOrder{};
+  const dim3 grid(a.max_splits, sh.Hkv, order.n ? order.n : a.max_seqs);
+  hipLaunchKernelGGL((attn_biased_kernel<R, 4, kMinWaves, PAGED, BYPOS, WEIGH>), grid, dim3(256), 0,
+                     s, a, b, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
+}
+
+template <typename R, bool PAGED>
+void launch_rows(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hipStream_t s) {
+  const bool by_position = b.slopes || b.window > 0;
+  if (b.weights) {
+    if (by_position) launch_biased<R, PAGED, true, true>(sh, a, b, s);
+    else launch_biased<R, PAGED, false, true>(sh, a, b, s);
+  } else {
+    if (by_position) launch_biased<R, PAGED, true, false>(sh, a, b, s);
+    else launch_biased<R, PAGED, false, false>(sh, a, b, s);
+  }
+}
+
+template <typename R>
+void launch_layout(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hipStream_t s) {
+  if (sh.pg.tables) launch_rows<R, true>(sh, a, b, s);
+  else launch_rows<R, false>(sh, a, b, s);
+}
+
+}  // namespace
+
+hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b,
+                                   hipStream_t s) {
+  if (sh.dtype == 2) launch_layout<E4m3Rows>(sh, a, b, s);
+  else if (sh.dtype == 1) launch_layout<Bf16Rows>(sh, a, b, s);
+  else launch_layout<F32Rows>(sh, a, b, s);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !b.weights) return e;
+  const int rows = a.max_splits * a.split_keys;
+  const int per = kWeighThreads * kWeighRows;
+  const dim3 grid((rows + per - 1) / per, sh.Hkv, a.max_seqs);
+  if (sh.pg.tables)
+    hipLaunchKernelGGL((add_weights_kernel<true>), grid, dim3(kWeighThreads), 0, s, a.meta, a.layer,
+                       b, sh.pg, sh.G, sh.Hq, sh.Hkv);
+  else
+    hipLaunchKernelGGL((add_weights_kernel<false>), grid, dim3(kWeighThreads), 0, s, a.meta,
+                       a.layer, b, sh.pg, sh.G, sh.Hq, sh.Hkv);
+  return hipGetLastError();
+}
+
+}  // namespace ra

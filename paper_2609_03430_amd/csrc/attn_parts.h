@@ -135,9 +135,14 @@ struct DenseSplits {
 // them (25 heads of 5,190 rows in 10 splits, G = 16: 27.6 -> 25.4 us).  Where the
 // workgroup has more threads than the head has channel pairs, the splits are
 // dealt to `parts` groups of threads, which merge in LDS in split order.
-template <typename E, int NT, typename Splits = DenseSplits>
+//
+// `stats(q, m, l)` is told the head's running maximum and sum of each query.
+struct NoStats {
+  __device__ __forceinline__ void operator()(int, float, float) const {}
+};
+template <typename E, int NT, typename Splits = DenseSplits, typename Stats = NoStats>
 __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
-                              const Splits& splits = Splits()) {
+                              const Splits& splits = Splits(), const Stats& stats = Stats()) {
   __shared__ Partial s_part[NT];
   __shared__ int last;
   const int slot = splits.slot(), g = blockIdx.y, head = slot * Hkv + g;
@@ -199,6 +204,9 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
   };
   const auto put = [&](int item, const Partial& p) {
     const float inv = 1.f / p.l;
+    if constexpr (!std::is_same_v<Stats, NoStats>) {
+      if (item % (kHeadDim / 2) == 0) stats(item / (kHeadDim / 2), p.m, p.l);
+    }
     if constexpr (sizeof(E) == 2) {
       *reinterpret_cast<uint32_t*>(out + 2 * item) =
           f32_to_bf16(p.o0 * inv) | static_cast<uint32_t>(f32_to_bf16(p.o1 * inv)) << 16;
@@ -347,13 +355,14 @@ struct RowChannels {
 // a whole head writes the normalised output, another one its partial (merged
 // by the head's last item, or with FUSED false by combine_kernel).
 template <typename E, int W, bool FUSED, typename Splits = DenseSplits,
-          typename Channels = RowChannels>
+          typename Channels = RowChannels, typename Stats = NoStats>
 __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, int wave,
                                             int qi, int grp, const Softmax& st, int G, int Hq, int Hkv,
                                             float (&s_m)[W][kMaxGroup],
                                             float (&s_l)[W][kMaxGroup],
                                             float (&s_o)[W][kMaxGroup][kHeadDim],
-                                            const Splits& splits = Splits()) {
+                                            const Splits& splits = Splits(),
+                                            const Stats& stats = Stats()) {
   const int head = w.slot * Hkv + w.g;
   const int64_t item = static_cast<int64_t>(head) * a.split_stride + w.split;
   E* out = static_cast<E*>(a.out);
@@ -381,6 +390,9 @@ __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, 
       o += s_o[v][q][c] * sc;
     }
     if (w.nsplit == 1) {
+      if constexpr (!std::is_same_v<Stats, NoStats>) {
+        if (c == 0) stats(q, mx, lsum);
+      }
       const int64_t idx_out = (static_cast<int64_t>(w.slot) * Hq + w.g * G + q) * kHeadDim + c;
       if constexpr (sizeof(E) == 2) out[idx_out] = f32_to_bf16(o / lsum);
       else out[idx_out] = o / lsum;
@@ -399,7 +411,7 @@ __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, 
     }
   }
   if constexpr (FUSED) {
-    if (w.nsplit > 1) merge_if_last<E, 64 * W>(a, G, Hq, Hkv, splits);
+    if (w.nsplit > 1) merge_if_last<E, 64 * W>(a, G, Hq, Hkv, splits, stats);
   }
 }
 

@@ -99,6 +99,11 @@ struct ra_cache {
   std::vector<ra::BoundsRange> ranges;   // a step's own, room for every slot and layer
   std::vector<int> stale_layers;         //   set aside when bounds are attached
 
+  // accumulated attention weights (ra_weights_attach): a float per pool row
+  float* weights = nullptr;
+  const ra::WeightHooks* weight_hooks = nullptr;
+  bool biased_step = false;              // the last attention launch carries no row moves
+
   ra::Shape shape() const {
     ra::Shape sh{cfg.num_layers, cfg.num_q_heads, cfg.num_kv_heads, G,
                  cfg.recent_r, cfg.evict_every, cfg.dtype, cfg.layout,

@@ -727,6 +727,47 @@ __global__ __launch_bounds__(NT) void move_chunks_kernel(
   }
 }
 
+// The moves of an event after a positions-only selection, as move_chunks_kernel's, where
+// the heads are many or short: one workgroup per head of the slots given.
+template <int NT, typename E, bool PAGED>
+__global__ __launch_bounds__(NT) void move_listed_kernel(
+    const SeqMeta* __restrict__ meta, E* __restrict__ kpool, E* __restrict__ vpool,
+    const int32_t* __restrict__ pos, int L, int Hkv, int slot_lo, DueList due, Paging pg) {
+  __shared__ int f[kMaxEvery];
+  __shared__ int src_of[chunk_rows<NT, E>()];
+  __shared__ int tbl[PAGED ? kMaxPagesLds : 1];
+  const int per_seq = L * Hkv;
+  const int at = static_cast<int>(blockIdx.x) / per_seq;
+  const int slot = due.n ? due.slot[at] : slot_lo + at;
+  const int lg = static_cast<int>(blockIdx.x) % per_seq;
+  const SeqMeta& M = meta[slot];
+  if (!M.active || !M.due) return;
+  const int old_len = M.plan_len, new_len = M.len, m = old_len - new_len;
+  if (m <= 0 || m > kMaxEvery) return;
+  const RegionRows rrow{M.base + static_cast<int64_t>(lg) * M.cap};
+  PagedRows prow{};
+  if constexpr (PAGED) {
+    const int32_t* table = pg.tables + static_cast<int64_t>(slot) * pg.pages_per_seq;
+    const int n_pages = (old_len + (1 << pg.page_shift) - 1) >> pg.page_shift;
+    for (int i = threadIdx.x; i < n_pages; i += NT) tbl[i] = table[i];
+    __syncthreads();
+    prow = PagedRows{tbl, pg.group_rows, static_cast<int64_t>(lg) << pg.page_shift,
+                     pg.page_shift};
+  }
+  for (int k = threadIdx.x; k < m; k += NT) {
+    if constexpr (PAGED) f[k] = pos[prow(new_len + k)] - k;
+    else f[k] = pos[rrow(new_len + k)] - k;
+  }
+  __syncthreads();
+  const int d0 = __builtin_amdgcn_readfirstlane(f[0]);
+  if constexpr (PAGED)
+    compact_rows<NT, E, false, PagedRows, false>(f, m, src_of, d0, new_len, old_len, prow, kpool,
+                                                 vpool, nullptr);
+  else
+    compact_rows<NT, E, false, RegionRows, false>(f, m, src_of, d0, new_len, old_len, rrow, kpool,
+                                                  vpool, nullptr);
+}
+
 // ---- e4m3 rows -----------------------------------------------------------------
 
 // Eight consecutive codes of a channel, from code `off` (0..7) of the sixteen
@@ -993,6 +1034,21 @@ void launch_chunks(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpoo
                      *sh.due, sh.pg, sh.move_sync);
 }
 
+template <typename E>
+void launch_listed(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                   const int32_t* pos, int slot_lo, int slot_hi, hipStream_t s) {
+  const DueList due = sh.due ? *sh.due : DueList{};
+  const dim3 grid((due.n ? due.n : slot_hi - slot_lo) * sh.L * sh.Hkv);
+  E* k = static_cast<E*>(kpool);
+  E* v = static_cast<E*>(vpool);
+  if (sh.pg.tables)
+    hipLaunchKernelGGL((move_listed_kernel<1024, E, true>), grid, dim3(1024), 0, s, meta, k, v,
+                       pos, sh.L, sh.Hkv, slot_lo, due, sh.pg);
+  else
+    hipLaunchKernelGGL((move_listed_kernel<1024, E, false>), grid, dim3(1024), 0, s, meta, k, v,
+                       pos, sh.L, sh.Hkv, slot_lo, due, sh.pg);
+}
+
 template <int NT, int KPT>
 void launch_ff(const Shape& sh, const SeqMeta* meta, int32_t* pos, int slot_lo, int slot_hi,
                int n_steps, int rows, hipStream_t s) {
@@ -1087,6 +1143,41 @@ hipError_t launch_evict(const Shape& sh, const SeqMeta* meta, void* kpool,
                              max_candidates, s, drops_out, drop_stride);
   return launch_mode<false>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi,
                             max_candidates, s, drops_out, drop_stride);
+}
+
+hipError_t launch_listed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                               const int32_t* pos, int slot_lo, int slot_hi, int max_candidates,
+                               hipStream_t s) {
+  // a workgroup to a chunk where that makes more workgroups: the moves are a launch of
+  // their own either way
+  int n_chunks = 0;
+  if (sh.move_sync && sh.due && sh.due->n > 0) {
+    const int64_t heads = static_cast<int64_t>(sh.due->n) * sh.L * sh.Hkv;
+    const int chunk = event_chunk_rows(sh.dtype);
+    const int64_t moved = static_cast<int64_t>(max_candidates) + sh.r;
+    const int64_t n = (moved + 7 + chunk - 1) / chunk;
+    if (heads <= sh.move_words && sh.every + 8 <= chunk && n > 1 && n <= kMaxChunks &&
+        heads * n <= 1024)
+      n_chunks = static_cast<int>(n);
+  }
+  const bool paged = sh.pg.tables != nullptr;
+  if (sh.dtype == 2) {
+    if (paged) launch_move_e4m3<true>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, n_chunks, s);
+    else launch_move_e4m3<false>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, n_chunks, s);
+  } else if (n_chunks > 0) {
+    if (sh.dtype == 1) {
+      if (paged) launch_chunks<uint16_t, true>(sh, meta, kpool, vpool, pos, n_chunks, s);
+      else launch_chunks<uint16_t, false>(sh, meta, kpool, vpool, pos, n_chunks, s);
+    } else {
+      if (paged) launch_chunks<float, true>(sh, meta, kpool, vpool, pos, n_chunks, s);
+      else launch_chunks<float, false>(sh, meta, kpool, vpool, pos, n_chunks, s);
+    }
+  } else if (sh.dtype == 1) {
+    launch_listed<uint16_t>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, s);
+  } else {
+    launch_listed<float>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, s);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_flush_pending(const Shape& sh, SeqMeta* meta, void* kpool, void* vpool,

@@ -301,6 +301,80 @@ hipError_t launch_attention_e4m3(const Shape& sh, const AttnLaunch& a, hipStream
 hipError_t launch_block_attention(const Shape& sh, const AttnLaunch& a, const BlockChoice& choice,
                                   hipStream_t s);
 
+// Attention whose scores follow a rule (attn_biased.hip): s = scale q.k, capped, less
+// slope * distance, and hidden past a window.
+struct BiasLaunch {
+  float scale = 0.f;
+  float cap = 0.f;                // 0: none
+  const float* slopes = nullptr;  // [Hq]
+  int window = 0;                 // 0: none
+  int prefix = 0;
+  bool ordered = true;            // rows lie in the order of their positions
+  // accumulated weights (null: none kept), a float per pool row; the scores of the
+  // attended rows, [max_seqs][Hq][score_stride] in log2 units, and each query's maximum
+  // and sum, [max_seqs][Hq][2]
+  float* weights = nullptr;
+  float* scores = nullptr;
+  int64_t score_stride = 0;
+  float* stats = nullptr;
+};
+// Blocks that may hold rows within the window: `head` leading ones, then those from block
+// head + shift on.  Positions ascend, so a row within the window is one of the `window`
+// last rows, and one below the prefix one of the `prefix` first.
+struct WindowBlocks {
+  int head, shift, n;
+};
+__device__ __host__ inline WindowBlocks window_blocks(int len, int window, int prefix) {
+  WindowBlocks b{0, 0, len / kBlockRows + 1};
+  if (window <= 0) return b;
+  const int first = len + 1 > window ? (len + 1 - window) / kBlockRows : 0;
+  const int lead = prefix / kBlockRows + (prefix % kBlockRows != 0);
+  b.head = first < lead ? first : lead;
+  b.shift = first - b.head;
+  b.n -= b.shift;
+  return b;
+}
+hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b,
+                                   hipStream_t s);
+
+// What an attached buffer of accumulated weights changes (api_biased.cpp sets these, so
+// that a cache without one asks for none of it): an event drops the candidates of least
+// weight and compacts the weights too; rows [from, to) of every head of a slot take the
+// weights src [L * Hkv][to - from], or 0.
+struct WeightHooks {
+  hipError_t (*event)(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                      int32_t* pos, float* weights, int slot_lo, int slot_hi, int max_candidates,
+                      bool positions_only, hipStream_t s);
+  hipError_t (*set)(const Shape& sh, const SeqMeta& M, int slot, int from, int to,
+                    const float* src, float* weights, hipStream_t s);
+};
+hipError_t launch_weight_event(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                               int32_t* pos, float* weights, int slot_lo, int slot_hi,
+                               int max_candidates, bool positions_only, hipStream_t s);
+hipError_t launch_set_weights(const Shape& sh, const SeqMeta& M, int slot, int from, int to,
+                              const float* src, float* weights, hipStream_t s);
+hipError_t launch_export_weights(const Shape& sh, const SeqMeta& M, int slot, int len,
+                                 const float* weights, float* out, hipStream_t s);
+// The row moves of an event whose selection left each head's drop list in its rows of
+// positions past the new length (evict.hip).
+hipError_t launch_listed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                               const int32_t* pos, int slot_lo, int slot_hi, int max_candidates,
+                               hipStream_t s);
+
+// Rotary positions (rotary.hip): pair i of half turns by position * turns[i].
+struct RotaryLaunch {
+  int half;            // pairs
+  int adjacent;        // pair i is channels 2i, 2i + 1 (0: i, i + half)
+  float magnitude;
+  double turns[kHeadDim / 2];
+};
+hipError_t launch_rotate_step(const SeqMeta* meta, int max_seqs, int dtype, int Hq, int Hkv,
+                              const RotaryLaunch& r, const void* q, const void* k, void* q_out,
+                              void* k_out, hipStream_t s);
+hipError_t launch_rotate_rows(int dtype, const RotaryLaunch& r, const void* x, void* out,
+                              int64_t heads, int rows, int first, const int32_t* positions,
+                              hipStream_t s);
+
 // The allocation-free attention's partials: a file-scope device array of
 // kNoAllocScratchBytes (attention.hip).  scratch_address returns its device
 // address on the current device, looked up once per device.
