@@ -522,6 +522,9 @@ def _own_steps_state(s, seed):
         ra.ra_seq_begin(s.cache.handle, i, n, int(seed) & 0xFFFFFFFF, i, k, v)
     if c["kind"] == "weighed":
         s.totals = [torch.empty(c["layers"], c["kv_heads"], n, device=_device()) for n in s.lens]
+    # a pass makes the same steps again: where the rule reads positions, its first one is
+    # given the slots' records (of steps made) as they are now
+    s.records = s.cache.meta.clone() if c["slopes"] or c["window"] else None
     s.graph = None
     if c["graph"]:
         ra.ra_graph_mode(s.cache.handle, True)
@@ -579,6 +582,8 @@ def _own_run(s):
         return s.out
     if c["kind"] == "event":
         return _own_event(s)
+    if s.records is not None:
+        s.cache.meta.copy_(s.records)
     if s.graph is not None:
         s.graph.replay()
         return s.out
