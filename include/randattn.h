@@ -525,8 +525,8 @@ ra_status ra_rotate_rows(const ra_rotary* rotary, int32_t dtype, const void* x, 
  * new row always is.  Of a cache whose rows lie in the order of their positions (all but
  * hole-fill) only the rows that may be within the window or the prefix are read. */
 typedef struct {
-  float scale;              /* finite, >= 0; 0: 1 / sqrt(head_dim) */
-  float cap;                /* finite, >= 0; 0: none */
+  float scale;              /* 0: 1 / sqrt(head_dim); else within [2^-40, 2^40] */
+  float cap;                /* 0: none; else within [2^-40, 2^40] */
   const float* dev_slopes;  /* [num_q_heads], or NULL: none */
   int32_t window;           /* >= 0; 0: none */
   int32_t prefix;           /* >= 0: positions that a window never hides */

@@ -1059,6 +1059,18 @@ ra_status ra_evict_now(ra_cache* c, int32_t seq, void* stream) {
 
 namespace {
 
+// Steps until the next trigger at which an active sequence evicts (the triggers before it
+// change nothing): runs of a fast forward end there, not at every trigger (4,144 steps
+// without an event: 3 launches, not 195).
+int steps_to_event(const ra_config& c, const SeqMeta& M) {
+  const int every = trigger_every(c);
+  if (every == 0) return INT32_MAX;
+  const int64_t full = static_cast<int64_t>(M.prompt_len) + M.k_keep + c.recent_r + 1 - M.len;
+  const int64_t first = every - M.step % every;
+  const int64_t later = full > first ? (full - first + every - 1) / every * every : 0;
+  return static_cast<int>(std::min<int64_t>(first + later, INT32_MAX));
+}
+
 // Whether a fast forward runs as one launch (evict.hip): where it holds an event
 // (one of 8 heads, 364 candidates: 9.4 us in one launch, 17 in three; of 288 heads,
 // 8,964 candidates: 52 and 55; eight: 40 and 88, 314 and 424; steps without one
@@ -1100,7 +1112,6 @@ ra_status fused_fast_forward(ra_cache* c, int lo, int hi, int n_steps, int rows,
 // ra_seq_fast_forward); the other slots' records and rows are not touched
 // (their deferred moves, if any, stay pending).
 ra_status fast_forward_range(ra_cache* c, int lo, int hi, int32_t n_steps, hipStream_t s) {
-  const int every = c->cfg.evict_every;
   bool pending = false;
   for (int i = lo; i < hi; ++i) pending = pending || c->mirror[i].due == ra::kDueMovePending;
   if (pending) {
@@ -1109,7 +1120,7 @@ ra_status fast_forward_range(ra_cache* c, int lo, int hi, int32_t n_steps, hipSt
   }
   for (int i = lo; i < hi; ++i)
     if (c->mirror[i].active) c->rows_change(i, c->mirror[i].prompt_len);
-  // Runs of steps up to the next trigger of any sequence.  The first pass
+  // Runs of steps up to the next event of any sequence.  The first pass
   // replays them on a copy of the mirror only, so that a capacity error (rows
   // piling up under the external policy) is reported before any launch; the
   // second pass launches and updates the mirror.
@@ -1132,8 +1143,7 @@ ra_status fast_forward_range(ra_cache* c, int lo, int hi, int32_t n_steps, hipSt
     while (remaining > 0 && hi > lo) {
       int run = remaining;
       for (int i = lo; i < hi; ++i)
-        if (c->mirror[i].active && trigger_every(c->cfg) > 0)
-          run = std::min(run, every - c->mirror[i].step % every);
+        if (c->mirror[i].active) run = std::min(run, steps_to_event(c->cfg, c->mirror[i]));
       if (c->is_paged()) {
         // pages for the run's rows
         int64_t short_groups = 0;

@@ -121,8 +121,9 @@ ra_status ra_rotate_rows(const ra_rotary* rotary, int32_t dtype, const void* x, 
 ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* rule, const void* q,
                               const void* k_new, const void* v_new, void* out, void* workspace,
                               size_t workspace_bytes, void* stream) {
-  if (!rule || !std::isfinite(rule->scale) || rule->scale < 0.f || !std::isfinite(rule->cap) ||
-      rule->cap < 0.f || rule->window < 0 || rule->prefix < 0)
+  // (factors whose quotients and products are normal numbers)
+  const auto usable = [](float x) { return x == 0.f || (x >= 0x1p-40f && x <= 0x1p40f); };
+  if (!rule || !usable(rule->scale) || !usable(rule->cap) || rule->window < 0 || rule->prefix < 0)
     return RA_ERR_INVALID_ARG;
   const ra_status st = ra::host::check_decode(c, layer, q, k_new, v_new, out);
   if (st != RA_OK) return st;
@@ -146,6 +147,7 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
           blocks, int64_t(window) / ra::kBlockRows + 2 + rule->prefix / ra::kBlockRows + 1);
     most = std::max(most, static_cast<int>(blocks));
   }
+  if (c->weights && score_rows > ra::kMaxScoreRows) return RA_ERR_UNSUPPORTED;
   const size_t need =
       c->weights ? weighed_bytes(c->cfg, score_rows) : ra_workspace_bytes(&c->cfg);
   if (!workspace || workspace_bytes < need || misaligned(workspace)) return RA_ERR_INVALID_ARG;
@@ -189,6 +191,7 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   b.window = rule->window;
   b.prefix = rule->prefix;
   b.ordered = ordered;
+  ra::score_units(b);
   if (c->weights) {
     b.weights = c->weights;
     b.stats = reinterpret_cast<float*>(static_cast<char*>(workspace) +

@@ -51,10 +51,15 @@ struct BiasedSplits {
   __device__ __forceinline__ int operator()(const AttnLaunch&, int) const { return n; }
 };
 
-// Each query's maximum and sum of a head, for add_weights_kernel.
-struct KeepStats {
+// The units of the scores; with KEEP each query's maximum and sum of a head, for
+// add_weights_kernel.
+template <bool KEEP>
+struct RuleEnds {
+  static constexpr bool kKeeps = KEEP;
+  float unit;
   float* to;       // [G][2]
-  __device__ __forceinline__ void operator()(int q, float m, float l) const {
+  __device__ __forceinline__ float log2(float x) const { return x * unit; }
+  __device__ __forceinline__ void keep(int q, float m, float l) const {
     to[2 * q] = m;
     to[2 * q + 1] = l;
   }
@@ -63,14 +68,40 @@ struct KeepStats {
 // tanh y, to about an ulp: up to 1 as y less a correction of at most a quarter of it,
 // tanh y = y - y^3 (45045 + 2772 y^2 + 27 y^4) / (135135 + 62370 y^2 + 3150 y^4 + 28 y^6)
 // (the convergent of its continued fraction y / (1 + y^2 / (3 + y^2 / (5 + ..))) that ends
-// with 13), past it as 1 - 2 / (1 + e^2y), where the quotient is a quarter at most.
+// with 13), past it as 1 - 2 / (1 + e^2y), where the quotient is a quarter at most.  Both are
+// made and one is taken: the empty asm keeps the compiler from branching around either,
+// sixteen times a block.
 __device__ __forceinline__ float tanh_of(float y) {
   const float a = fabsf(y), y2 = y * y;
   const float num = 45045.f + y2 * (2772.f + y2 * 27.f);
   const float den = 135135.f + y2 * (62370.f + y2 * (3150.f + y2 * 28.f));
-  const float near = y - y * y2 * num * __builtin_amdgcn_rcpf(den);
-  const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_fast(a * (2.f * kLog2e)));
+  float near = y - y * y2 * num * __builtin_amdgcn_rcpf(den);
+  float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + exp2_fast(a * (2.f * kLog2e)));
+  asm("" : "+v"(near), "+v"(far));
   return a > 1.f ? copysignf(far, y) : near;
+}
+
+// First pool row of a cached block.  The tables do not change while the kernel runs, and
+// their entries come by scalar loads: a vector load, which the compiler takes because the
+// kernel also stores, would wait for every row in flight (192 heads of 6,200 paged e4m3
+// rows, with weights: 154 us).
+template <bool PAGED>
+__device__ __forceinline__ int64_t block_row(const RowMap& m, int block) {
+  if constexpr (PAGED) {
+    typedef const int32_t __attribute__((address_space(4)))* ConstantTable;
+    const int j = __builtin_amdgcn_readfirstlane(block) * kBlockRows;
+    const int64_t page = ((ConstantTable)(reinterpret_cast<uintptr_t>(m.table)))[j >> m.page_shift];
+    return page * m.group_rows + m.head_off + (j & ((1 << m.page_shift) - 1));
+  } else {
+    return m.region + block * kBlockRows;
+  }
+}
+
+// 16 bytes at an offset of a buffer, dropped past its end.
+__device__ __forceinline__ void store16(__amdgpu_buffer_rsrc_t to, uint32_t offset, float a,
+                                        float b, float c, float d) {
+  const u32x4 v = {__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
+  __builtin_amdgcn_raw_buffer_store_b128(v, to, static_cast<int>(offset), 0, 0);
 }
 
 // The four wavefronts of a workgroup and their register buffers as in attn_blocks_kernel.
@@ -84,7 +115,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   using Two = typename R::New::Two;
   __shared__ float s_m[W][kMaxGroup];
   __shared__ float s_l[W][kMaxGroup];
-  __shared__ float s_o[W][kMaxGroup][kHeadDim];
+  __shared__ __align__(16) float s_o[W][kMaxGroup][kHeadDim];
   __shared__ __align__(16) typename R::New s_new;
   const BiasedWork w = locate_biased(a, bias, order, Hkv, pg);
   if (!w.valid) return;
@@ -97,10 +128,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   const int b1 = __builtin_amdgcn_readfirstlane(min(b0 + per, w.b1));
   const bool has = b0 < b1;
   const bool owns_last = has && b1 == w.win.n;
-  const float slope = BYPOS && bias.slopes && qi < G ? bias.slopes[w.g * G + qi] * kLog2e : 0.f;
-  const float scale_log2 = bias.scale * kLog2e;
-  const float cap_log2 = bias.cap * kLog2e;
-  const float to_cap = bias.cap > 0.f ? bias.scale / bias.cap : 0.f;
+  const float slope = BYPOS && bias.slopes && qi < G ? bias.slopes[w.g * G + qi] : 0.f;
 
   struct Buffer {
     typename R::Block rows;
@@ -108,7 +136,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   };
   const auto load = [&](Buffer& b, int i) {
     const int cached = i < w.win.head ? i : i + w.win.shift;
-    const int64_t row = pool_row<PAGED>(w.rm, cached * kBlockRows);
+    const int64_t row = block_row<PAGED>(w.rm, cached);
     R::load(b.rows, pools, row, lm);
     if constexpr (BYPOS) {
       const u32x4 lo = ld16(a.pos + row + lm.vrow), hi = ld16(a.pos + row + lm.vrow + 4);
@@ -119,10 +147,11 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
       }
     }
   };
-  float* scores = nullptr;
-  if constexpr (WEIGH)
-    scores = bias.scores + (static_cast<int64_t>(w.slot) * Hq + w.g * G + qi) * bias.score_stride +
-             8 * grp;
+  // the scores of the head's queries, [block][G][32]
+  const auto scores = __builtin_amdgcn_make_buffer_rsrc(
+      bias.scores + (static_cast<int64_t>(w.slot) * Hq + w.g * G) * bias.score_stride, 0,
+      static_cast<int>(4u * static_cast<uint32_t>(G * bias.score_stride)), 0x00020000);
+  const uint32_t q_offset = 4u * static_cast<uint32_t>(kBlockRows * qi + 8 * grp);
 
   Softmax st;
   st.m = kNoScore;
@@ -158,17 +187,18 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
       R::scores(b.rows, q, x);
       if (bias.cap > 0.f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = cap_log2 * tanh_of(x[e] * to_cap);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= scale_log2;
+        for (int e = 0; e < 8; ++e) x[e] = tanh_of(x[e] * bias.before);
       }
       if constexpr (BYPOS) {
+        if (bias.slopes) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = x[e] * bias.after - slope * static_cast<float>(w.now - b.p[e]);
+        }
         uint32_t hidden = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int dist = w.now - b.p[e];
-          x[e] -= slope * static_cast<float>(dist);
           if (bias.window > 0 && dist >= bias.window && b.p[e] >= bias.prefix) {
             x[e] = kNegInf;
             hidden |= 1u << e;
@@ -183,13 +213,13 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
           if (8 * grp + e >= limit) x[e] = kNegInf;
       }
       if constexpr (WEIGH) {
-        if (qi < G) {
-          f32x4* to = reinterpret_cast<f32x4*>(scores + static_cast<int64_t>(i) * kBlockRows);
-          to[0] = f32x4{x[0], x[1], x[2], x[3]};
-          to[1] = f32x4{x[4], x[5], x[6], x[7]};
-        }
+        // (lanes of no query write past the buffer's end, which drops them: a store that some
+        // of them branched around would leave the loads in flight behind it uncounted)
+        const uint32_t at = qi < G ? q_offset + 4u * (kBlockRows * G * i) : ~31u;
+        store16(scores, at, x[0], x[1], x[2], x[3]);
+        store16(scores, at + 16u, x[4], x[5], x[6], x[7]);
       }
-      R::attend(st, b.rows, x);
+      R::attend(st, b.rows, x, bias.unit);
     };
     // two register buffers in turn; every prefetch is issued (the last block's again
     // once there is none left), so that the wait for a block leaves the next one's
@@ -222,14 +252,10 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   }
   if constexpr (std::is_same_v<R, E4m3Rows>) R::gather_channels(st);
   const BiasedSplits splits{w.slot, w.nsplit};
-  if constexpr (WEIGH) {
-    const KeepStats keep{bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G)};
-    finish_item<E, W, true, BiasedSplits, typename R::Channels>(
-        a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits, keep);
-  } else {
-    finish_item<E, W, true, BiasedSplits, typename R::Channels>(
-        a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits);
-  }
+  RuleEnds<WEIGH> ends{bias.unit, nullptr};
+  if constexpr (WEIGH) ends.to = bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G);
+  finish_item<E, W, true, BiasedSplits, typename R::Channels>(
+      a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits, ends);
   if (owns_last) {
     const int64_t row = pool_row<PAGED>(w.rm, w.len);
     s_new.append(a, row, k_scale, v_scale);
@@ -256,17 +282,18 @@ __global__ __launch_bounds__(kWeighThreads) void add_weights_kernel(const SeqMet
   const int j = (i < win.head ? i : i + win.shift) * kBlockRows + at % kBlockRows;
   if (j > len) return;
   const int64_t head = static_cast<int64_t>(slot) * Hq + g * G;
-  const float* s = bias.scores + head * bias.score_stride + at;
+  const float* s = bias.scores + head * bias.score_stride + static_cast<int64_t>(i) * G * kBlockRows +
+                   at % kBlockRows;
   const float* st = bias.stats + 2 * head;
   const RowMap rm = row_map(M, slot, layer * Hkv + g, pg);
   f32x4* to = reinterpret_cast<f32x4*>(bias.weights + pool_row<PAGED>(rm, j));
   f32x4 w = *to, sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int q = 0; q < G; ++q) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(s + q * bias.score_stride);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(s + q * kBlockRows);
     const float m = st[2 * q], inv = 1.f / st[2 * q + 1];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += exp2f(x[e] - m) * inv;
+    for (int e = 0; e < 4; ++e) sum[e] += exp2_fast((x[e] - m) * bias.unit) * inv;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = j + e < len ? w[e] + sum[e] : j + e == len ? sum[e] : w[e];

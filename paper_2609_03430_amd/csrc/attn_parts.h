@@ -136,13 +136,16 @@ struct DenseSplits {
 // workgroup has more threads than the head has channel pairs, the splits are
 // dealt to `parts` groups of threads, which merge in LDS in split order.
 //
-// `stats(q, m, l)` is told the head's running maximum and sum of each query.
-struct NoStats {
-  __device__ __forceinline__ void operator()(int, float, float) const {}
+// `ends` says what the maxima are in (log2(x): a difference of two in log2 units), and where
+// it keeps them is told the head's maximum and sum of each query.
+struct Log2Ends {
+  static constexpr bool kKeeps = false;
+  __device__ __forceinline__ float log2(float x) const { return x; }
+  __device__ __forceinline__ void keep(int, float, float) const {}
 };
-template <typename E, int NT, typename Splits = DenseSplits, typename Stats = NoStats>
+template <typename E, int NT, typename Splits = DenseSplits, typename Ends = Log2Ends>
 __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
-                              const Splits& splits = Splits(), const Stats& stats = Stats()) {
+                              const Splits& splits = Splits(), const Ends& ends = Ends()) {
   __shared__ Partial s_part[NT];
   __shared__ int last;
   const int slot = splits.slot(), g = blockIdx.y, head = slot * Hkv + g;
@@ -183,14 +186,14 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
       float mx = p.m;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) mx = fmaxf(mx, m[j]);
-      const float keep = exp2f(p.m - mx);
+      const float keep = exp2f(ends.log2(p.m - mx));
       p.m = mx;
       p.l *= keep;
       p.o0 *= keep;
       p.o1 *= keep;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const float w = s0 + j < hi ? exp2f(m[j] - mx) : 0.f;
+        const float w = s0 + j < hi ? exp2f(ends.log2(m[j] - mx)) : 0.f;
         p.l += w * l[j];
         p.o0 += w * x[j];
         p.o1 += w * y[j];
@@ -204,8 +207,8 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
   };
   const auto put = [&](int item, const Partial& p) {
     const float inv = 1.f / p.l;
-    if constexpr (!std::is_same_v<Stats, NoStats>) {
-      if (item % (kHeadDim / 2) == 0) stats(item / (kHeadDim / 2), p.m, p.l);
+    if constexpr (Ends::kKeeps) {
+      if (item % (kHeadDim / 2) == 0) ends.keep(item / (kHeadDim / 2), p.m, p.l);
     }
     if constexpr (sizeof(E) == 2) {
       *reinterpret_cast<uint32_t*>(out + 2 * item) =
@@ -231,7 +234,8 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
     Partial p = s_part[t];
     for (int k = 1; k < parts && k * per < nsplit; ++k) {
       const Partial r = s_part[k * pairs + t];
-      const float mx = fmaxf(p.m, r.m), wp = exp2f(p.m - mx), wr = exp2f(r.m - mx);
+      const float mx = fmaxf(p.m, r.m);
+      const float wp = exp2f(ends.log2(p.m - mx)), wr = exp2f(ends.log2(r.m - mx));
       p = Partial{mx, p.l * wp + r.l * wr, p.o0 * wp + r.o0 * wr, p.o1 * wp + r.o1 * wr};
     }
     put(t, p);
@@ -279,7 +283,7 @@ __device__ __forceinline__ void load_block(BlockRegs& b, const uint16_t* Kr,
 }
 
 struct Softmax {
-  float m;      // running max of the scaled scores (log2 units), per query
+  float m;      // running max of the scores (log2 units, unless said otherwise), per query
   float l;      // this lane's share of the running sum
   f32x4 acc[8]; // O^T tile u: channels 16u + 4*grp + i, query lane & 15
 };
@@ -355,14 +359,14 @@ struct RowChannels {
 // a whole head writes the normalised output, another one its partial (merged
 // by the head's last item, or with FUSED false by combine_kernel).
 template <typename E, int W, bool FUSED, typename Splits = DenseSplits,
-          typename Channels = RowChannels, typename Stats = NoStats>
+          typename Channels = RowChannels, typename Ends = Log2Ends>
 __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, int wave,
                                             int qi, int grp, const Softmax& st, int G, int Hq, int Hkv,
                                             float (&s_m)[W][kMaxGroup],
                                             float (&s_l)[W][kMaxGroup],
                                             float (&s_o)[W][kMaxGroup][kHeadDim],
                                             const Splits& splits = Splits(),
-                                            const Stats& stats = Stats()) {
+                                            const Ends& ends = Ends()) {
   const int head = w.slot * Hkv + w.g;
   const int64_t item = static_cast<int64_t>(head) * a.split_stride + w.split;
   E* out = static_cast<E*>(a.out);
@@ -385,13 +389,13 @@ __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, 
     float lsum = 0.f, o = 0.f;
 #pragma unroll
     for (int v = 0; v < W; ++v) {
-      const float sc = exp2f(s_m[v][q] - mx);
+      const float sc = exp2f(ends.log2(s_m[v][q] - mx));
       lsum += s_l[v][q] * sc;
       o += s_o[v][q][c] * sc;
     }
     if (w.nsplit == 1) {
-      if constexpr (!std::is_same_v<Stats, NoStats>) {
-        if (c == 0) stats(q, mx, lsum);
+      if constexpr (Ends::kKeeps) {
+        if (c == 0) ends.keep(q, mx, lsum);
       }
       const int64_t idx_out = (static_cast<int64_t>(w.slot) * Hq + w.g * G + q) * kHeadDim + c;
       if constexpr (sizeof(E) == 2) out[idx_out] = f32_to_bf16(o / lsum);
@@ -411,7 +415,7 @@ __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, 
     }
   }
   if constexpr (FUSED) {
-    if (w.nsplit > 1) merge_if_last<E, 64 * W>(a, G, Hq, Hkv, splits, stats);
+    if (w.nsplit > 1) merge_if_last<E, 64 * W>(a, G, Hq, Hkv, splits, ends);
   }
 }
 

@@ -1,7 +1,7 @@
 // Cached rows of each dtype as the attention kernels take them, blocks of 32 at a time: a
 // lane's loads of a block, the step's new pair in its place, the scores of the block's
-// keys (x[e]: key 8 * (lane >> 4) + e) and its values weighed by them (log2 units; -inf: a
-// masked key).
+// keys (x[e]: key 8 * (lane >> 4) + e) and its values weighed by them (a difference of two
+// scores times `unit` is one in log2 units; -inf: a masked key).
 #pragma once
 
 #include "attn_parts.h"
@@ -108,22 +108,20 @@ struct Bf16Rows {
       x[4 + i] = s1[i];
     }
   }
-  static __device__ __forceinline__ void attend(Softmax& st, const Block& b,
-                                                const float (&x)[8]) {
+  static __device__ __forceinline__ void attend(Softmax& st, const Block& b, const float (&x)[8],
+                                                float unit) {
     float bm = x[0];
   #pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
-    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
-    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-    const float mn = fmaxf(st.m, bm);
-    const float alpha = exp2f(st.m - mn);
+    const float mn = fmaxf(st.m, max_over_groups(bm));
+    const float alpha = exp2_fast((st.m - mn) * unit);
     // P = hi + lo, both bf16, so the weights keep ~16 significant bits through
     // the bf16 MFMA (the remainder of a bf16 rounding is exact in fp32)
     bf16x8 p_hi, p_lo;
     float psum = 0.f;
   #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float pf = exp2f(x[e] - mn);
+      const float pf = exp2_fast((x[e] - mn) * unit);
       const __bf16 hi = static_cast<__bf16>(pf);
       p_hi[e] = hi;
       p_lo[e] = static_cast<__bf16>(pf - static_cast<float>(hi));
@@ -330,19 +328,19 @@ struct E4m3Rows {
       x[4 + i] = s[1][i];
     }
   }
-  static __device__ __forceinline__ void attend(Softmax& st, const Block& b,
-                                                const float (&x)[8]) {
+  static __device__ __forceinline__ void attend(Softmax& st, const Block& b, const float (&x)[8],
+                                                float unit) {
     float bm = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
     const float mn = fmaxf(st.m, max_over_groups(bm));
-    const float alpha = exp2_fast(st.m - mn);
+    const float alpha = exp2_fast((st.m - mn) * unit);
     // weights times their values' scales as hi + lo, both bf16 (16 significant bits)
     bf16x8 p_hi, p_lo;
     float psum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float pf = exp2_fast(x[e] - mn);
+      const float pf = exp2_fast((x[e] - mn) * unit);
       const uint32_t w = static_cast<uint32_t>(b.vs >> (32 * (e >> 2)));
       const float pv = pf * e4m3_scale(w >> (8 * (e & 3)) & 255u);
       const __bf16 hi = static_cast<__bf16>(pv);
@@ -376,7 +374,7 @@ struct E4m3Rows {
       for (int e = 0; e < 8; ++e)
         if (8 * grp + e >= limit) x[e] = kNegInf;
     }
-    attend(st, b, x);
+    attend(st, b, x, 1.f);
   }
   // The values of the keys whose bit is set in `hidden` (of the lane's eight) as zeros.
   static __device__ __forceinline__ void hide(Block& b, uint32_t hidden) {
@@ -506,17 +504,17 @@ struct F32Rows {
       x[4 + i] = s[1][i];
     }
   }
-  static __device__ __forceinline__ void attend(Softmax& st, const Block& b,
-                                                const float (&x)[8]) {
+  static __device__ __forceinline__ void attend(Softmax& st, const Block& b, const float (&x)[8],
+                                                float unit) {
     float bm = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
     const float mn = fmaxf(st.m, max_over_groups(bm));
-    const float alpha = exp2f(st.m - mn);
+    const float alpha = exp2_fast((st.m - mn) * unit);
     float p[8], psum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[e] = exp2f(x[e] - mn);
+      p[e] = exp2_fast((x[e] - mn) * unit);
       psum += p[e];
     }
     st.l = st.l * alpha + psum;

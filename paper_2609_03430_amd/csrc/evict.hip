@@ -727,47 +727,6 @@ __global__ __launch_bounds__(NT) void move_chunks_kernel(
   }
 }
 
-// The moves of an event after a positions-only selection, as move_chunks_kernel's, where
-// the heads are many or short: one workgroup per head of the slots given.
-template <int NT, typename E, bool PAGED>
-__global__ __launch_bounds__(NT) void move_listed_kernel(
-    const SeqMeta* __restrict__ meta, E* __restrict__ kpool, E* __restrict__ vpool,
-    const int32_t* __restrict__ pos, int L, int Hkv, int slot_lo, DueList due, Paging pg) {
-  __shared__ int f[kMaxEvery];
-  __shared__ int src_of[chunk_rows<NT, E>()];
-  __shared__ int tbl[PAGED ? kMaxPagesLds : 1];
-  const int per_seq = L * Hkv;
-  const int at = static_cast<int>(blockIdx.x) / per_seq;
-  const int slot = due.n ? due.slot[at] : slot_lo + at;
-  const int lg = static_cast<int>(blockIdx.x) % per_seq;
-  const SeqMeta& M = meta[slot];
-  if (!M.active || !M.due) return;
-  const int old_len = M.plan_len, new_len = M.len, m = old_len - new_len;
-  if (m <= 0 || m > kMaxEvery) return;
-  const RegionRows rrow{M.base + static_cast<int64_t>(lg) * M.cap};
-  PagedRows prow{};
-  if constexpr (PAGED) {
-    const int32_t* table = pg.tables + static_cast<int64_t>(slot) * pg.pages_per_seq;
-    const int n_pages = (old_len + (1 << pg.page_shift) - 1) >> pg.page_shift;
-    for (int i = threadIdx.x; i < n_pages; i += NT) tbl[i] = table[i];
-    __syncthreads();
-    prow = PagedRows{tbl, pg.group_rows, static_cast<int64_t>(lg) << pg.page_shift,
-                     pg.page_shift};
-  }
-  for (int k = threadIdx.x; k < m; k += NT) {
-    if constexpr (PAGED) f[k] = pos[prow(new_len + k)] - k;
-    else f[k] = pos[rrow(new_len + k)] - k;
-  }
-  __syncthreads();
-  const int d0 = __builtin_amdgcn_readfirstlane(f[0]);
-  if constexpr (PAGED)
-    compact_rows<NT, E, false, PagedRows, false>(f, m, src_of, d0, new_len, old_len, prow, kpool,
-                                                 vpool, nullptr);
-  else
-    compact_rows<NT, E, false, RegionRows, false>(f, m, src_of, d0, new_len, old_len, rrow, kpool,
-                                                  vpool, nullptr);
-}
-
 // ---- e4m3 rows -----------------------------------------------------------------
 
 // Eight consecutive codes of a channel, from code `off` (0..7) of the sixteen
@@ -941,6 +900,75 @@ __global__ __launch_bounds__(NT) void move_e4m3_kernel(
   }
 }
 
+// The moves of an event by weight, after its selection (weights.hip): rows of any dtype, of
+// any number of slots.  A workgroup per head, or with CHUNKED one per chunk of rows, handed
+// over as in move_chunks_kernel; a head's sync word is the weight of the first row that the
+// event frees, which the selection has cleared.
+template <int NT, typename E, bool PAGED, bool CHUNKED>
+__global__ __launch_bounds__(NT) void move_weighed_kernel(
+    const SeqMeta* __restrict__ meta, E* __restrict__ kpool, E* __restrict__ vpool,
+    uint8_t* __restrict__ kscale, uint8_t* __restrict__ vscale, const int32_t* __restrict__ pos,
+    float* weights, int L, int Hkv, int n_chunks, int slot_lo, DueList due, Paging pg) {
+  constexpr int kDtype = sizeof(E) == 4 ? 0 : sizeof(E) == 2 ? 1 : 2;
+  constexpr int kChunk = event_chunk_rows(kDtype);
+  __shared__ int f[kMaxEvery];
+  __shared__ int src_of[kChunk];
+  __shared__ int tbl[PAGED ? kMaxPagesLds : 1];
+  __shared__ int s_chunk;
+  const int per_seq = L * Hkv;
+  const int head = static_cast<int>(blockIdx.x) / n_chunks;
+  const int slot = due.n ? due.slot[head / per_seq] : slot_lo + head / per_seq;
+  const int lg = head % per_seq;
+  const SeqMeta& M = meta[slot];
+  if (!M.active || !M.due) return;
+  const int old_len = M.plan_len, new_len = M.len, m = old_len - new_len;
+  if (m <= 0 || m > kMaxEvery) return;
+  const int t = threadIdx.x;
+  uint32_t* word = reinterpret_cast<uint32_t*>(weights) +
+                   pool_row<PAGED>(row_map(M, slot, lg, pg), new_len);
+  if (CHUNKED && t == 0)
+    s_chunk = static_cast<int>(
+        __hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & 31u);
+  const RegionRows rrow{M.base + static_cast<int64_t>(lg) * M.cap};
+  PagedRows prow{};
+  if constexpr (PAGED) {
+    const int32_t* table = pg.tables + static_cast<int64_t>(slot) * pg.pages_per_seq;
+    const int n_pages = (old_len + (1 << pg.page_shift) - 1) >> pg.page_shift;
+    for (int i = t; i < n_pages; i += NT) tbl[i] = table[i];
+    __syncthreads();
+    prow = PagedRows{tbl, pg.group_rows, static_cast<int64_t>(lg) << pg.page_shift,
+                     pg.page_shift};
+  }
+  for (int k = t; k < m; k += NT) {
+    if constexpr (PAGED) f[k] = pos[prow(new_len + k)] - k;
+    else f[k] = pos[rrow(new_len + k)] - k;
+  }
+  __syncthreads();
+  const int chunk = CHUNKED ? __builtin_amdgcn_readfirstlane(s_chunk) : 0;
+  const int d0 = __builtin_amdgcn_readfirstlane(f[0]);
+  const int j0 = (d0 & ~7) + chunk * kChunk;
+  if (j0 >= new_len) return;
+  const int first = max(d0, j0), end = CHUNKED ? min(new_len, j0 + kChunk) : new_len;
+  const auto move = [&](const auto& loaded) {
+    if constexpr (kDtype == 2 && PAGED)
+      compact_rows_e4m3<NT, kChunk>(f, m, src_of, first, end, old_len, prow, kpool, vpool, kscale,
+                                    vscale, loaded);
+    else if constexpr (kDtype == 2)
+      compact_rows_e4m3<NT, kChunk>(f, m, src_of, first, end, old_len, rrow, kpool, vpool, kscale,
+                                    vscale, loaded);
+    else if constexpr (PAGED)
+      compact_rows<NT, E, false, PagedRows, false>(f, m, src_of, first, end, old_len, prow, kpool,
+                                                   vpool, nullptr, loaded);
+    else
+      // (the region is a multiple of a value tile: the rows count from it)
+      compact_rows<NT, E, false, RegionRows, false>(
+          f, m, src_of, first, end, old_len, RegionRows{0}, kpool + rrow.region * kHeadDim,
+          vpool + rrow.region * kHeadDim, nullptr, loaded);
+  };
+  if constexpr (CHUNKED) move(ChunkLoaded{word, chunk});
+  else move(NoHook{});
+}
+
 template <bool PAGED>
 void launch_move_e4m3(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
                       const int32_t* pos, int slot_lo, int slot_hi, int n_chunks, hipStream_t s) {
@@ -1032,21 +1060,6 @@ void launch_chunks(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpoo
   hipLaunchKernelGGL((move_chunks_kernel<1024, E, PAGED>), grid, dim3(1024), 0, s, meta,
                      static_cast<E*>(kpool), static_cast<E*>(vpool), pos, sh.L, sh.Hkv, n_chunks,
                      *sh.due, sh.pg, sh.move_sync);
-}
-
-template <typename E>
-void launch_listed(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
-                   const int32_t* pos, int slot_lo, int slot_hi, hipStream_t s) {
-  const DueList due = sh.due ? *sh.due : DueList{};
-  const dim3 grid((due.n ? due.n : slot_hi - slot_lo) * sh.L * sh.Hkv);
-  E* k = static_cast<E*>(kpool);
-  E* v = static_cast<E*>(vpool);
-  if (sh.pg.tables)
-    hipLaunchKernelGGL((move_listed_kernel<1024, E, true>), grid, dim3(1024), 0, s, meta, k, v,
-                       pos, sh.L, sh.Hkv, slot_lo, due, sh.pg);
-  else
-    hipLaunchKernelGGL((move_listed_kernel<1024, E, false>), grid, dim3(1024), 0, s, meta, k, v,
-                       pos, sh.L, sh.Hkv, slot_lo, due, sh.pg);
 }
 
 template <int NT, int KPT>
@@ -1145,38 +1158,47 @@ hipError_t launch_evict(const Shape& sh, const SeqMeta* meta, void* kpool,
                             max_candidates, s, drops_out, drop_stride);
 }
 
-hipError_t launch_listed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
-                               const int32_t* pos, int slot_lo, int slot_hi, int max_candidates,
-                               hipStream_t s) {
-  // a workgroup to a chunk where that makes more workgroups: the moves are a launch of
-  // their own either way
-  int n_chunks = 0;
-  if (sh.move_sync && sh.due && sh.due->n > 0) {
-    const int64_t heads = static_cast<int64_t>(sh.due->n) * sh.L * sh.Hkv;
-    const int chunk = event_chunk_rows(sh.dtype);
-    const int64_t moved = static_cast<int64_t>(max_candidates) + sh.r;
-    const int64_t n = (moved + 7 + chunk - 1) / chunk;
-    if (heads <= sh.move_words && sh.every + 8 <= chunk && n > 1 && n <= kMaxChunks &&
-        heads * n <= 1024)
-      n_chunks = static_cast<int>(n);
-  }
-  const bool paged = sh.pg.tables != nullptr;
-  if (sh.dtype == 2) {
-    if (paged) launch_move_e4m3<true>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, n_chunks, s);
-    else launch_move_e4m3<false>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, n_chunks, s);
-  } else if (n_chunks > 0) {
-    if (sh.dtype == 1) {
-      if (paged) launch_chunks<uint16_t, true>(sh, meta, kpool, vpool, pos, n_chunks, s);
-      else launch_chunks<uint16_t, false>(sh, meta, kpool, vpool, pos, n_chunks, s);
-    } else {
-      if (paged) launch_chunks<float, true>(sh, meta, kpool, vpool, pos, n_chunks, s);
-      else launch_chunks<float, false>(sh, meta, kpool, vpool, pos, n_chunks, s);
-    }
-  } else if (sh.dtype == 1) {
-    launch_listed<uint16_t>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, s);
+namespace {
+
+template <typename E>
+void launch_weighed(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                    const int32_t* pos, float* weights, int slot_lo, int slot_hi, int n_chunks,
+                    hipStream_t s) {
+  const DueList due = sh.due ? *sh.due : DueList{};
+  const int heads = (due.n ? due.n : slot_hi - slot_lo) * sh.L * sh.Hkv;
+  E* k = static_cast<E*>(kpool);
+  E* v = static_cast<E*>(vpool);
+#define RA_MOVE(PAGED, CHUNKED, CHUNKS)                                                          \
+  hipLaunchKernelGGL((move_weighed_kernel<1024, E, PAGED, CHUNKED>), dim3(heads * (CHUNKS)),     \
+                     dim3(1024), 0, s, meta, k, v, sh.k_scale, sh.v_scale, pos, weights, sh.L,   \
+                     sh.Hkv, CHUNKS, slot_lo, due, sh.pg)
+  if (n_chunks > 1) {
+    if (sh.pg.tables) RA_MOVE(true, true, n_chunks);
+    else RA_MOVE(false, true, n_chunks);
   } else {
-    launch_listed<float>(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, s);
+    if (sh.pg.tables) RA_MOVE(true, false, 1);
+    else RA_MOVE(false, false, 1);
   }
+#undef RA_MOVE
+}
+
+}  // namespace
+
+hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                                const int32_t* pos, float* weights, int slot_lo, int slot_hi,
+                                int max_candidates, hipStream_t s) {
+  // rows move down by less than a chunk: an event drops up to `every` rows, but under the
+  // external policy, whose rows pile up
+  const int chunk = event_chunk_rows(sh.dtype);
+  const int64_t n = (static_cast<int64_t>(max_candidates) + sh.r + 7 + chunk - 1) / chunk;
+  const int n_chunks =
+      sh.policy != 4 && sh.every + 8 <= chunk && n <= kMaxChunks ? static_cast<int>(n) : 1;
+  if (sh.dtype == 2)
+    launch_weighed<uint8_t>(sh, meta, kpool, vpool, pos, weights, slot_lo, slot_hi, n_chunks, s);
+  else if (sh.dtype == 1)
+    launch_weighed<uint16_t>(sh, meta, kpool, vpool, pos, weights, slot_lo, slot_hi, n_chunks, s);
+  else
+    launch_weighed<float>(sh, meta, kpool, vpool, pos, weights, slot_lo, slot_hi, n_chunks, s);
   return hipGetLastError();
 }
 

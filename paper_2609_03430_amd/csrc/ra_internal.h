@@ -310,14 +310,29 @@ struct BiasLaunch {
   int window = 0;                 // 0: none
   int prefix = 0;
   bool ordered = true;            // rows lie in the order of their positions
+  // what the kernel keeps the scores in: a difference of two times `unit` is one in log2
+  // units (see score_units)
+  float unit = 1.f;
+  float before = 1.f;             // q.k times this: the cap's argument
+  float after = 1.f;              // .. and the score times this: what is kept
   // accumulated weights (null: none kept), a float per pool row; the scores of the
-  // attended rows, [max_seqs][Hq][score_stride] in log2 units, and each query's maximum
-  // and sum, [max_seqs][Hq][2]
+  // attended rows, [max_seqs][Hq][score_stride], and each query's maximum and sum,
+  // [max_seqs][Hq][2]
   float* weights = nullptr;
   float* scores = nullptr;
   int64_t score_stride = 0;
   float* stats = nullptr;
 };
+// Scores stay as the products (or tanh of them) give them until a difference is taken, so
+// that no rounding of a score of 40 weighs in its exponential; slopes take them in natural
+// units first.
+inline void score_units(BiasLaunch& b) {
+  const float log2e = 1.4426950408889634f;
+  const float own = b.cap > 0.f ? b.cap : b.scale;
+  b.before = b.cap > 0.f ? b.scale / b.cap : 1.f;
+  b.after = b.slopes ? own : 1.f;
+  b.unit = b.slopes ? log2e : own * log2e;
+}
 // Blocks that may hold rows within the window: `head` leading ones, then those from block
 // head + shift on.  Positions ascend, so a row within the window is one of the `window`
 // last rows, and one below the prefix one of the `prefix` first.
@@ -334,6 +349,7 @@ __device__ __host__ inline WindowBlocks window_blocks(int len, int window, int p
   b.n -= b.shift;
   return b;
 }
+constexpr int64_t kMaxScoreRows = int64_t(1) << 25;   // a head's scores are one buffer
 hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b,
                                    hipStream_t s);
 
@@ -355,11 +371,11 @@ hipError_t launch_set_weights(const Shape& sh, const SeqMeta& M, int slot, int f
                               const float* src, float* weights, hipStream_t s);
 hipError_t launch_export_weights(const Shape& sh, const SeqMeta& M, int slot, int len,
                                  const float* weights, float* out, hipStream_t s);
-// The row moves of an event whose selection left each head's drop list in its rows of
-// positions past the new length (evict.hip).
-hipError_t launch_listed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
-                               const int32_t* pos, int slot_lo, int slot_hi, int max_candidates,
-                               hipStream_t s);
+// The row moves of an event by weight whose selection left each head's drop list in its rows
+// of positions past the new length, and 0 in the weight of the first of them (evict.hip).
+hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                                const int32_t* pos, float* weights, int slot_lo, int slot_hi,
+                                int max_candidates, hipStream_t s);
 
 // Rotary positions (rotary.hip): pair i of half turns by position * turns[i].
 struct RotaryLaunch {

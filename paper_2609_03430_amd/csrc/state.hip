@@ -25,7 +25,7 @@ __global__ void seq_set_kernel(SeqMeta* meta, int slot, SeqMeta v) {
 }
 
 // Applies the trigger rule to a sequence that has just completed `n_steps`
-// more steps (n_steps never crosses a multiple of `every` before its end).
+// more steps (none before the last at which it would evict).
 __device__ __forceinline__ void plan(SeqMeta& M, int r, bool at_trigger) {
   M.due = 0;
   if (at_trigger && M.len - M.prompt_len - r > M.k_keep) {

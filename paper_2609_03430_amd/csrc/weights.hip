@@ -5,7 +5,7 @@
 // recent), the m of least weight, the earliest first among equal ones (select.h, on the
 // weights' bits).  One workgroup per head selects and compacts positions and weights, and
 // leaves its drop list in the m rows of positions that the compaction frees; the key and
-// value rows move in a second launch (launch_listed_moves), so the selection's registers
+// value rows move in a second launch (launch_weighed_moves), so the selection's registers
 // and the moves' do not add up.
 #include "ra_internal.h"
 #include "select.h"
@@ -123,8 +123,10 @@ __global__ __launch_bounds__(NT) void weight_event_kernel(const SeqMeta* __restr
       weights[to] = wj;
     }
   }
-  // the drop list, in rows that every thread has read by now
+  // the drop list, and a word for the moves to order themselves by, in rows that every thread
+  // has read by now
   __syncthreads();
+  if (t == 0) weights[row(new_len)] = 0.f;
   for (int i = t; i < m; i += NT) pos[row(new_len + i)] = f[i] + i;
 }
 
@@ -193,7 +195,7 @@ hipError_t launch_weight_event(const Shape& sh, const SeqMeta* meta, void* kpool
 #undef RA_SELECT
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || positions_only) return e;
-  return launch_listed_moves(sh, meta, kpool, vpool, pos, slot_lo, slot_hi, max_candidates, s);
+  return launch_weighed_moves(sh, meta, kpool, vpool, pos, weights, slot_lo, slot_hi, max_candidates, s);
 }
 
 hipError_t launch_set_weights(const Shape& sh, const SeqMeta& M, int slot, int from, int to,

@@ -189,6 +189,7 @@ def test_states_and_refusals():
     assert status(B.ra_write_weights, h, 2, w) == A
     assert status(B.ra_write_weights, h, 1, w) == S           # inactive
     for kw in (dict(scale=-1.0), dict(scale=float("nan")), dict(cap=-1.0), dict(cap=float("inf")),
+               dict(scale=1e-20), dict(cap=1e20), dict(cap=float("nan")),
                dict(window=-1), dict(prefix=-1)):
         assert status(c.decode_biased, 0, B.make_score_rule(**kw), q, k, k, out) == A, kw
     short = B.make_score_rule(slopes=torch.zeros(1, device=DEV))
