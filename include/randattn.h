@@ -485,7 +485,7 @@ typedef enum {
 
 typedef struct {
   double base;           /* > 1 */
-  double factor;         /* > 0, unless RA_ROTARY_PLAIN */
+  double factor;         /* >= 1, unless RA_ROTARY_PLAIN */
   double low, high;      /* ROTATIONS and CHANNELS: 0 < low < high, in turns */
   double magnitude;      /* m, which the turned channels are multiplied by; 0 counts as 1 */
   int32_t dims;          /* even, in [2, 128] */

@@ -38,7 +38,7 @@ size_t weighed_bytes(const ra_config& c, int64_t rows) {
          (stats_floats(c) + static_cast<size_t>(c.max_seqs) * c.num_q_heads * rows) * sizeof(float);
 }
 
-// Turns per position of every pair, or an error.
+// Quarter turns per position of every pair (at most 2 / pi: base > 1, factor >= 1), or an error.
 ra_status rotary_turns(const ra_rotary* p, ra::RotaryLaunch& out) {
   if (!p || p->dims < 2 || p->dims > ra::kHeadDim || p->dims % 2 != 0 ||
       !(std::isfinite(p->base) && p->base > 1.0) ||
@@ -46,7 +46,7 @@ ra_status rotary_turns(const ra_rotary* p, ra::RotaryLaunch& out) {
       p->scaling < RA_ROTARY_PLAIN || p->scaling > RA_ROTARY_CHANNELS ||
       !std::isfinite(p->magnitude) || p->magnitude < 0.0)
     return RA_ERR_INVALID_ARG;
-  if (p->scaling != RA_ROTARY_PLAIN && !(std::isfinite(p->factor) && p->factor > 0.0))
+  if (p->scaling != RA_ROTARY_PLAIN && !(std::isfinite(p->factor) && p->factor >= 1.0))
     return RA_ERR_INVALID_ARG;
   const bool bands = p->scaling == RA_ROTARY_ROTATIONS || p->scaling == RA_ROTARY_CHANNELS;
   if (bands && !(p->original_len > 0 && std::isfinite(p->high) && p->low > 0.0 && p->high > p->low))
@@ -76,9 +76,26 @@ ra_status rotary_turns(const ra_rotary* p, ra::RotaryLaunch& out) {
     }
     own = std::min(1.0, std::max(0.0, own));
     const double scaled = p->scaling == RA_ROTARY_PLAIN ? f : f * (own + (1.0 - own) / p->factor);
-    out.turns[i] = i < out.half ? scaled / pi2 : 0.0;
+    out.quarters[i] = i < out.half ? scaled / (pi2 / 4) : 0.0;
   }
   return RA_OK;
+}
+
+// plan_blocks, but for few fp32 rows, twice as long as those it was measured with: 64 keys to
+// a workgroup while there is a CU for each, and no more than 512 (microseconds per layer in a
+// captured step, plan_blocks and this: 2 heads of 200 rows 13.3 and 10.5, of 500 15.0 and
+// 11.9; 8 heads of 600 17.4 and 13.8, of 9,000 35.0 and 30.3; but 64 heads of 600, 640
+// workgroups, 20.4 and 35.3; 8 of 2,200 stay at 19.5, with 64 keys 26.5).
+Plan biased_plan(const ra_cache* c, int64_t keys_max, int heads) {
+  Plan p = ra::host::plan_blocks(c, keys_max, heads);
+  if (c->cfg.dtype != RA_F32 || c->cfg.attn_split > 0) return p;
+  const auto items = [&](int64_t keys) { return (keys_max + keys - 1) / keys; };
+  int keys = p.split_keys;
+  if (keys_max <= 1000 && items(64) * heads <= 256) keys = 64;
+  else if (items(512) * heads <= 256 && items(512) <= ra::kMaxSplits) keys = std::min(keys, 512);
+  p.split_keys = keys;
+  p.max_splits = p.partials = static_cast<int>(items(keys));
+  return p;
 }
 
 }  // namespace
@@ -163,8 +180,8 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   ++c->n_appended;
   c->biased_step = true;
   if (n_active == 0) return RA_OK;
-  const Plan plan = ra::host::plan_blocks(c, int64_t(most) * ra::kBlockRows,
-                                          n_active * c->cfg.num_kv_heads);
+  const Plan plan =
+      biased_plan(c, int64_t(most) * ra::kBlockRows, n_active * c->cfg.num_kv_heads);
   const size_t items = static_cast<size_t>(c->cfg.max_seqs) * c->cfg.num_kv_heads * ra::kMaxSplits;
   ra::AttnLaunch a{};
   a.meta = c->meta;

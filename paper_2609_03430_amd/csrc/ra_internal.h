@@ -377,12 +377,13 @@ hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpoo
                                 const int32_t* pos, float* weights, int slot_lo, int slot_hi,
                                 int max_candidates, hipStream_t s);
 
-// Rotary positions (rotary.hip): pair i of half turns by position * turns[i].
+// Rotary positions (rotary.hip): pair i of `half` turns by position * quarters[i] quarter
+// turns, which fit 31 bits.
 struct RotaryLaunch {
   int half;            // pairs
   int adjacent;        // pair i is channels 2i, 2i + 1 (0: i, i + half)
   float magnitude;
-  double turns[kHeadDim / 2];
+  double quarters[kHeadDim / 2];
 };
 hipError_t launch_rotate_step(const SeqMeta* meta, int max_seqs, int dtype, int Hq, int Hkv,
                               const RotaryLaunch& r, const void* q, const void* k, void* q_out,

@@ -1,8 +1,7 @@
 // Rotary positions: the pairs of a row's leading channels turned by the row's position.
-//   a' = m (a cos - b sin),  b' = m (b cos + a sin),  angle = position * turns[pair]
+//   a' = m (a cos - b sin),  b' = m (b cos + a sin),  angle = position * quarters[pair], in quarter turns
 // The angle of a far position has more whole turns than fp32 has digits to spare: the
-// product and its remainder are taken in 64 bits, the sine and cosine of what is left, an
-// eighth of a turn at most, in 32.
+// product and its remainder are taken in 64 bits, the sine and cosine of the rest in 32.
 #include "attn_parts.h"
 
 namespace ra {
@@ -12,14 +11,19 @@ struct SinCos {
   float s, c;
 };
 
-__device__ __forceinline__ SinCos turned(double turns, float magnitude) {
-  const double quarters = rint(4.0 * turns);
-  const float x = static_cast<float>(2.0 * (turns - 0.25 * quarters));   // half turns
-  float s, c;
-  sincospif(x, &s, &c);
-  const int q = static_cast<int>(static_cast<int64_t>(quarters) & 3);
+// Of an angle in quarter turns: the nearest whole quarter, whose sine and cosine swap and
+// negate those of what is left, an eighth of a turn at most to either side.  There the series
+// of sine and cosine end with the ninth and the tenth power (what is cut off is below 2^-28).
+__device__ __forceinline__ SinCos turned(double quarters, float magnitude) {
+  const double whole = rint(quarters);
+  const float x = static_cast<float>(quarters - whole) * 1.57079632679489662f, y = x * x;
+  const float s =
+      x + x * y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880))));
+  const float c =
+      1.f + y * (-0.5f + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320 - y * (1.f / 3628800)))));
+  const int q = static_cast<int>(whole);
   const float a = q & 1 ? c : s, b = q & 1 ? s : c;
-  return {magnitude * (q & 2 ? -a : a), magnitude * ((q == 1 || q == 2) ? -b : b)};
+  return {magnitude * (q & 2 ? -a : a), magnitude * ((q + 1) & 2 ? -b : b)};
 }
 
 __device__ __forceinline__ float to_f32(uint16_t x) {
@@ -29,14 +33,13 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ void put(uint16_t& to, float x) { to = f32_to_bf16(x); }
 __device__ __forceinline__ void put(float& to, float x) { to = x; }
 
-// A thread's part of a row: eight pairs, or sixteen of the channels that stay.  PACKED:
-// pairs in whole 16-byte units (half a multiple of 8), eight threads to a row; otherwise
-// one pair, 64 threads.
+// A thread's part of a row: with PACKED the pairs of two 16-byte units (eight of bf16, four
+// of fp32: half is a multiple of that), otherwise one pair; past them as many of the channels
+// that stay.
 template <typename E, bool ADJACENT, bool PACKED>
 struct Part {
-  static constexpr int kPairs = PACKED ? 8 : 1;
+  static constexpr int kPairs = PACKED ? 16 / static_cast<int>(sizeof(E)) : 1;
   static constexpr int kLanes = kHeadDim / 2 / kPairs;
-  static constexpr int kUnits = kPairs * sizeof(E) / 16;   // 16-byte loads of each side
   int ca, cb;          // first channels of the two sides
   int pair;            // first pair
   bool turns;
@@ -57,13 +60,9 @@ struct Part {
   };
   __device__ __forceinline__ void load(Regs& x, const E* row) const {
     if constexpr (PACKED) {
-#pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        const u32x4 a = ld16(row + ca + i * (16 / sizeof(E)));
-        const u32x4 b = ld16(row + cb + i * (16 / sizeof(E)));
-        __builtin_memcpy(x.a + i * (16 / sizeof(E)), &a, 16);
-        __builtin_memcpy(x.b + i * (16 / sizeof(E)), &b, 16);
-      }
+      const u32x4 a = ld16(row + ca), b = ld16(row + cb);
+      __builtin_memcpy(x.a, &a, 16);
+      __builtin_memcpy(x.b, &b, 16);
     } else {
       x.a[0] = row[ca];
       x.b[0] = row[cb];
@@ -71,14 +70,11 @@ struct Part {
   }
   __device__ __forceinline__ void store(const Regs& x, E* row) const {
     if constexpr (PACKED) {
-#pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        u32x4 a, b;
-        __builtin_memcpy(&a, x.a + i * (16 / sizeof(E)), 16);
-        __builtin_memcpy(&b, x.b + i * (16 / sizeof(E)), 16);
-        *reinterpret_cast<u32x4*>(row + ca + i * (16 / sizeof(E))) = a;
-        *reinterpret_cast<u32x4*>(row + cb + i * (16 / sizeof(E))) = b;
-      }
+      u32x4 a, b;
+      __builtin_memcpy(&a, x.a, 16);
+      __builtin_memcpy(&b, x.b, 16);
+      *reinterpret_cast<u32x4*>(row + ca) = a;
+      *reinterpret_cast<u32x4*>(row + cb) = b;
     } else {
       row[ca] = x.a[0];
       row[cb] = x.b[0];
@@ -89,7 +85,7 @@ struct Part {
     if (!turns) return;
 #pragma unroll
     for (int i = 0; i < kPairs; ++i)
-      sc[i] = turned(static_cast<double>(position) * r.turns[pair + i], r.magnitude);
+      sc[i] = turned(static_cast<double>(position) * r.quarters[pair + i], r.magnitude);
   }
   __device__ __forceinline__ void rotate(Regs& x, const SinCos (&sc)[kPairs]) const {
     if (!turns) return;
@@ -167,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(RotaryLaunch r, c
 // f(Part): the build for the rows' type, the pairs' layout and their number.
 template <typename E, typename F>
 void with_part(const RotaryLaunch& r, F&& f) {
-  if (r.half % 8 == 0) {
+  if (r.half % (16 / static_cast<int>(sizeof(E))) == 0) {
     if (r.adjacent) f(std::true_type{}, std::true_type{});
     else f(std::false_type{}, std::true_type{});
   } else {
@@ -197,7 +193,10 @@ void rotate_rows(const RotaryLaunch& r, const void* x, void* out, int64_t heads,
     constexpr bool kAdjacent = decltype(adjacent)::value, kPacked = decltype(packed)::value;
     const int tile = kThreads / Part<E, kAdjacent, kPacked>::kLanes;
     const unsigned tiles = static_cast<unsigned>((static_cast<int64_t>(rows) + tile - 1) / tile);
-    const int per = 8;
+    // heads to a workgroup: up to eight, which share their angles, while the workgroups are many
+    // (50 fp32 heads of 2,113 rows, positions of their own: 8 heads 27 us)
+    const int64_t all = heads * tiles / 4096;
+    const int per = positions || all < 1 ? 1 : all < 8 ? static_cast<int>(all) : 8;
     const int64_t runs = (heads + per - 1) / per;
     hipLaunchKernelGGL((rotate_rows_kernel<E, kAdjacent, kPacked>),
                        dim3(tiles, static_cast<unsigned>(runs < 65535 ? runs : 65535)),

@@ -52,7 +52,7 @@ def test_null_handles_are_refused():
     dict(base=1.0), dict(base=float("nan")), dict(base=float("inf")), dict(base=-5.0), dict(dims=0),
     dict(dims=3), dict(dims=130), dict(dims=-2), dict(pairs=2), dict(pairs=-1), dict(scaling=4),
     dict(scaling=-1), dict(magnitude=-1.0), dict(magnitude=float("nan")),
-    dict(scaling=1, factor=0.0), dict(scaling=1, factor=float("inf")),
+    dict(scaling=1, factor=0.5), dict(scaling=1, factor=float("inf")),
     dict(scaling=2, low=4.0, high=4.0), dict(scaling=2, low=0.0), dict(scaling=2, original_len=0),
     dict(scaling=3, high=float("inf")), dict(scaling=3, low=float("nan")),
     dict(scaling=3, original_len=-1),

@@ -91,6 +91,17 @@ def test_long_heads_in_splits(dtype, G):
         sim.close()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_head_of_more_rows_than_its_splits_hold_at_512(dtype):
+    """One head of 33,000 rows (65 splits of 512) and a short one beside it."""
+    for n in ([33000], [33000, 100]):
+        sim = Sim(1, 2, 1, 0, n, r=0, every=64, dtype=dtype)
+        kw = dict(cap=30.0)
+        sim.step(sim.rule(kw), kw)
+        sim.check()
+        sim.close()
+
+
 @pytest.mark.parametrize("window,prefix", [(1, 0), (1, 40), (32, 0), (33, 32), (2 ** 31 - 1, 0),
                                            (97, 2 ** 31 - 1), (64, 1)])
 def test_window_edges(window, prefix):
