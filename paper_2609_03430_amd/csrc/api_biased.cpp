@@ -81,19 +81,28 @@ ra_status rotary_turns(const ra_rotary* p, ra::RotaryLaunch& out) {
   return RA_OK;
 }
 
-// plan_blocks, but for few fp32 rows, twice as long as those it was measured with: 64 keys to
-// a workgroup while there is a CU for each, and no more than 512 (microseconds per layer in a
-// captured step, plan_blocks and this: 2 heads of 200 rows 13.3 and 10.5, of 500 15.0 and
-// 11.9; 8 heads of 600 17.4 and 13.8, of 9,000 35.0 and 30.3; but 64 heads of 600, 640
-// workgroups, 20.4 and 35.3; 8 of 2,200 stay at 19.5, with 64 keys 26.5).
-Plan biased_plan(const ra_cache* c, int64_t keys_max, int heads) {
+// plan_blocks, but for two kinds of launches (microseconds per layer in a captured step,
+// plan_blocks and this):
+//   few fp32 rows, twice as long as those it was measured with: 64 keys to a workgroup while
+//     there is a CU for each, and no more than 512 (2 heads of 200 rows 13.3 and 10.5, of 500
+//     15.0 and 11.9; 8 heads of 600 17.4 and 13.8, of 9,000 35.0 and 30.3; but 64 heads of
+//     600, 640 workgroups, 20.4 and 35.3; 8 of 2,200 stay at 19.5, with 64 keys 26.5);
+//   129 to 256 ragged heads, of which it makes one item each: six, so that the CUs of the short
+//     ones share the long ones' work (bf16, 160 heads of 300 to 9,000 rows 199 and 95, 256 of
+//     them 217 and 142, 192 of 4,500 to 9,000 226 and 148, of 200 to 3,000 69 and 43; e4m3, 192
+//     of 300 to 9,000 100 and 55, of 200 to 3,000 42 and 29; four items within 15% of it).
+Plan biased_plan(const ra_cache* c, int64_t keys_max, int64_t keys_mean, int heads) {
   Plan p = ra::host::plan_blocks(c, keys_max, heads);
-  if (c->cfg.dtype != RA_F32 || c->cfg.attn_split > 0) return p;
+  if (c->cfg.attn_split > 0) return p;
   const auto items = [&](int64_t keys) { return (keys_max + keys - 1) / keys; };
-  int keys = p.split_keys;
-  if (keys_max <= 1000 && items(64) * heads <= 256) keys = 64;
-  else if (items(512) * heads <= 256 && items(512) <= ra::kMaxSplits) keys = std::min(keys, 512);
-  p.split_keys = keys;
+  int64_t keys = p.split_keys;
+  if (c->cfg.dtype == RA_F32 && keys_max <= 1000 && items(64) * heads <= 256)
+    keys = 64;
+  else if (c->cfg.dtype == RA_F32 && items(512) * heads <= 256 && items(512) <= ra::kMaxSplits)
+    keys = std::min<int64_t>(keys, 512);
+  else if (heads > 128 && heads <= 256 && keys_max >= 1536 && 8 * keys_mean < 7 * keys_max)
+    keys = ra::host::round_up((keys_max + 5) / 6, ra::kBlockRows);
+  p.split_keys = static_cast<int>(keys);
   p.max_splits = p.partials = static_cast<int>(items(keys));
   return p;
 }
@@ -148,21 +157,22 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   const bool ordered = c->cfg.layout != RA_LAYOUT_HOLE_FILL;
   const int window = ordered ? rule->window : 0;
   int most = 0, n_active = 0;
+  int64_t blocks_all = 0;
   int64_t score_rows = c->is_paged() ? paged_rows(c->cfg) : ra::kRegionAlign;
   for (int s = c->slot_lo; s < c->slot_hi; ++s) {
     const SeqMeta& M = c->mirror[s];
     if (!M.active) continue;
     ++n_active;
     if (!c->is_paged()) score_rows = std::max<int64_t>(score_rows, M.cap);
-    if (!c->graph) {
-      most = std::max(most, ra::window_blocks(M.len, window, rule->prefix).n);
-      continue;
+    int64_t blocks = ra::window_blocks(M.len, window, rule->prefix).n;
+    if (c->graph) {
+      blocks = M.cap / ra::kBlockRows;
+      if (window > 0)
+        blocks = std::min<int64_t>(
+            blocks, int64_t(window) / ra::kBlockRows + 2 + rule->prefix / ra::kBlockRows + 1);
     }
-    int64_t blocks = M.cap / ra::kBlockRows;
-    if (window > 0)
-      blocks = std::min<int64_t>(
-          blocks, int64_t(window) / ra::kBlockRows + 2 + rule->prefix / ra::kBlockRows + 1);
     most = std::max(most, static_cast<int>(blocks));
+    blocks_all += blocks;
   }
   if (c->weights && score_rows > ra::kMaxScoreRows) return RA_ERR_UNSUPPORTED;
   const size_t need =
@@ -181,7 +191,8 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   c->biased_step = true;
   if (n_active == 0) return RA_OK;
   const Plan plan =
-      biased_plan(c, int64_t(most) * ra::kBlockRows, n_active * c->cfg.num_kv_heads);
+      biased_plan(c, int64_t(most) * ra::kBlockRows, blocks_all * ra::kBlockRows / n_active,
+                  n_active * c->cfg.num_kv_heads);
   const size_t items = static_cast<size_t>(c->cfg.max_seqs) * c->cfg.num_kv_heads * ra::kMaxSplits;
   ra::AttnLaunch a{};
   a.meta = c->meta;

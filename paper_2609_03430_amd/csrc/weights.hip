@@ -131,21 +131,19 @@ __global__ __launch_bounds__(NT) void weight_event_kernel(const SeqMeta* __restr
 }
 
 // Rows [from, from + n) of every head: their weights set from src [L * Hkv][n] (null: 0),
-// or with out, copied there.  Grid: (runs of 1,024 rows, L * Hkv).
-constexpr int kCopyThreads = 256, kCopyRows = 1024;
+// or with out, copied there.  A row to a thread: a copy's time is the latency of a load and a
+// store.  Grid: (runs of 256 rows, L * Hkv).
+constexpr int kCopyRows = 256;
 template <bool PAGED>
-__global__ __launch_bounds__(kCopyThreads) void copy_weights_kernel(
+__global__ __launch_bounds__(kCopyRows) void copy_weights_kernel(
     SeqMeta M, int slot, int from, int n, Paging pg, const float* src, float* weights, float* out) {
+  const int j = blockIdx.x * kCopyRows + threadIdx.x;
+  if (j >= n) return;
   const RowMap rm = row_map(M, slot, blockIdx.y, pg);
-  const int64_t at = static_cast<int64_t>(blockIdx.y) * n;
-#pragma unroll
-  for (int i = 0; i < kCopyRows / kCopyThreads; ++i) {
-    const int j = blockIdx.x * kCopyRows + i * kCopyThreads + threadIdx.x;
-    if (j >= n) return;
-    const int64_t row = pool_row<PAGED>(rm, from + j);
-    if (out) out[at + j] = weights[row];
-    else weights[row] = src ? src[at + j] : 0.f;
-  }
+  const int64_t at = static_cast<int64_t>(blockIdx.y) * n + j;
+  const int64_t row = pool_row<PAGED>(rm, from + j);
+  if (out) out[at] = weights[row];
+  else weights[row] = src ? src[at] : 0.f;
 }
 
 hipError_t copy_weights(const Shape& sh, const SeqMeta& M, int slot, int from, int n,
@@ -153,10 +151,10 @@ hipError_t copy_weights(const Shape& sh, const SeqMeta& M, int slot, int from, i
   if (n <= 0) return hipSuccess;
   const dim3 grid((n + kCopyRows - 1) / kCopyRows, sh.L * sh.Hkv);
   if (sh.pg.tables)
-    hipLaunchKernelGGL((copy_weights_kernel<true>), grid, dim3(kCopyThreads), 0, s, M, slot, from,
+    hipLaunchKernelGGL((copy_weights_kernel<true>), grid, dim3(kCopyRows), 0, s, M, slot, from,
                        n, sh.pg, src, weights, out);
   else
-    hipLaunchKernelGGL((copy_weights_kernel<false>), grid, dim3(kCopyThreads), 0, s, M, slot, from,
+    hipLaunchKernelGGL((copy_weights_kernel<false>), grid, dim3(kCopyRows), 0, s, M, slot, from,
                        n, sh.pg, src, weights, out);
   return hipGetLastError();
 }
