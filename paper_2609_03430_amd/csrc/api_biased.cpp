@@ -179,9 +179,15 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
       c->weights ? weighed_bytes(c->cfg, score_rows) : ra_workspace_bytes(&c->cfg);
   if (!workspace || workspace_bytes < need || misaligned(workspace)) return RA_ERR_INVALID_ARG;
   const hipStream_t hs = static_cast<hipStream_t>(stream);
-  // the rows of deferred events move first: this attention moves none
-  const ra_status fl = ra::host::flush_pending(c, hs);
-  if (fl != RA_OK) return fl;
+  // the rows of deferred events move first, as this attention moves none: every layer's at
+  // once, or where layers of this step have moved theirs (each while it attended) this one's
+  if (c->n_appended == 0) {
+    const ra_status fl = ra::host::flush_pending(c, hs);
+    if (fl != RA_OK) return fl;
+  } else if (c->any_pending()) {
+    RA_LAUNCH(ra::launch_flush_layer(c->shape(), c->meta, c->kpool, c->vpool, c->drops,
+                                     c->cfg.evict_every, layer, c->slot_lo, c->slot_hi, hs));
+  }
   const ra_status grown = ra::host::grow_for_step(c, hs);
   if (grown != RA_OK) return grown;
   ra::Shape sh = c->shape();

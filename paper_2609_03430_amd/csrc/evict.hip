@@ -634,6 +634,27 @@ __global__ __launch_bounds__(NT) void move_pending_kernel(
                                                 RegionRows{region}, kpool, vpool, nullptr);
 }
 
+// The same for one layer of a step whose earlier layers moved theirs while they attended.
+template <int NT, typename E>
+__global__ __launch_bounds__(NT) void move_pending_layer_kernel(
+    const SeqMeta* __restrict__ meta, E* __restrict__ kpool, E* __restrict__ vpool,
+    const int32_t* __restrict__ drops, int stride, int layer, int L, int Hkv, int slot_lo) {
+  __shared__ int f[kMaxEvery];
+  __shared__ int src_of[chunk_rows<NT, E>()];
+  const int slot = slot_lo + static_cast<int>(blockIdx.x) / Hkv;
+  const int lg = layer * Hkv + static_cast<int>(blockIdx.x) % Hkv;
+  const SeqMeta& M = meta[slot];
+  if (!M.active || M.due != kDueMovePending) return;
+  const int old_len = M.plan_len, new_len = M.len, m = old_len - new_len;
+  if (m <= 0 || m > stride) return;
+  const int32_t* d = drops + (static_cast<int64_t>(slot) * L * Hkv + lg) * stride;
+  for (int k = threadIdx.x; k < m; k += NT) f[k] = d[k] - k;
+  __syncthreads();
+  const int64_t region = M.base + static_cast<int64_t>(lg) * M.cap;
+  compact_rows<NT, E, false, RegionRows, false>(f, m, src_of, f[0], new_len, old_len,
+                                                RegionRows{region}, kpool, vpool, nullptr);
+}
+
 // The moves of an event whose due heads are fewer than the CUs, after a
 // positions-only selection that left each head's drop list in its rows of
 // positions past the new length.  Every chunk of chunk_rows destination rows
@@ -1158,6 +1179,22 @@ hipError_t launch_evict(const Shape& sh, const SeqMeta* meta, void* kpool,
                             max_candidates, s, drops_out, drop_stride);
 }
 
+hipError_t launch_flush_layer(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                              const int32_t* drops, int drop_stride, int layer, int slot_lo,
+                              int slot_hi, hipStream_t s) {
+  if (sh.dtype != 1) return hipErrorInvalidValue;   // (only bf16 events defer their moves)
+  const int chunk = std::max(1, (1 << 20) / sh.Hkv);
+  for (int a = slot_lo; a < slot_hi; a += chunk) {
+    const int b = std::min(slot_hi, a + chunk);
+    hipLaunchKernelGGL((move_pending_layer_kernel<1024, uint16_t>), dim3((b - a) * sh.Hkv),
+                       dim3(1024), 0, s, meta, static_cast<uint16_t*>(kpool),
+                       static_cast<uint16_t*>(vpool), drops, drop_stride, layer, sh.L, sh.Hkv, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 namespace {
 
 template <typename E>
@@ -1191,8 +1228,12 @@ hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpoo
   // external policy, whose rows pile up
   const int chunk = event_chunk_rows(sh.dtype);
   const int64_t n = (static_cast<int64_t>(max_candidates) + sh.r + 7 + chunk - 1) / chunk;
-  const int n_chunks =
-      sh.policy != 4 && sh.every + 8 <= chunk && n <= kMaxChunks ? static_cast<int>(n) : 1;
+  const int64_t heads =
+      static_cast<int64_t>(sh.due && sh.due->n ? sh.due->n : slot_hi - slot_lo) * sh.L * sh.Hkv;
+  const int n_chunks = sh.policy != 4 && sh.every + 8 <= chunk && n <= kMaxChunks &&
+                               heads * n <= (1 << 20)
+                           ? static_cast<int>(n)
+                           : 1;
   if (sh.dtype == 2)
     launch_weighed<uint8_t>(sh, meta, kpool, vpool, pos, weights, slot_lo, slot_hi, n_chunks, s);
   else if (sh.dtype == 1)

@@ -194,6 +194,11 @@ hipError_t launch_clear_pending(SeqMeta* meta, int slot_lo, int slot_hi, hipStre
 hipError_t launch_flush_pending(const Shape& sh, SeqMeta* meta, void* kpool, void* vpool,
                                 const int32_t* drops, int drop_stride, int slot_lo,
                                 int slot_hi, hipStream_t s);
+// launch_flush_pending for one layer of the step that is open, the slots' flags left as they
+// are: earlier layers have moved their rows already.
+hipError_t launch_flush_layer(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
+                              const int32_t* drops, int drop_stride, int layer, int slot_lo,
+                              int slot_hi, hipStream_t s);
 // Rows [0, len) of every head of slot `slot` (host mirror M) from row-major
 // sources [L * Hkv][len][128] (positions: pos_src, or 0..len-1 if null).
 hipError_t launch_write_rows(const Shape& sh, const SeqMeta& M, int slot, int len,

@@ -105,6 +105,9 @@ struct Part {
 
 constexpr int kThreads = 256;
 
+// Workgroups of a launch, which go over more in turn: a grid holds 2^32 threads.
+unsigned workgroups(int64_t n) { return static_cast<unsigned>(n < (1 << 20) ? n : 1 << 20); }
+
 // A step's queries and keys, [max_seqs][Hq][128] and [max_seqs][Hkv][128], at the next
 // position of each active slot, which the slot records hold.
 template <typename E, bool ADJACENT, bool PACKED>
@@ -114,23 +117,26 @@ __global__ __launch_bounds__(kThreads) void rotate_step_kernel(const SeqMeta* me
                                                                E* k_out) {
   using P = Part<E, ADJACENT, PACKED>;
   const int heads = Hq + Hkv;
-  const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / P::kLanes;
-  const int slot = static_cast<int>(item / heads), h = static_cast<int>(item % heads);
-  if (slot >= max_seqs) return;
-  const bool is_q = h < Hq;
-  const E* src = is_q ? q : k;
-  if (!src) return;
-  const int64_t row = is_q ? static_cast<int64_t>(slot) * Hq + h
-                           : static_cast<int64_t>(slot) * Hkv + h - Hq;
   const P part(threadIdx.x % P::kLanes, r.half);
-  typename P::Regs x;
-  part.load(x, src + row * kHeadDim);
-  const SeqMeta& M = meta[slot];
-  if (!M.active) return;
-  SinCos sc[P::kPairs];
-  part.angles(sc, r, M.prompt_len + M.step);
-  part.rotate(x, sc);
-  part.store(x, (is_q ? q_out : k_out) + row * kHeadDim);
+  const int64_t items = static_cast<int64_t>(max_seqs) * heads;
+  constexpr int kPer = kThreads / P::kLanes;
+  for (int64_t item = static_cast<int64_t>(blockIdx.x) * kPer + threadIdx.x / P::kLanes;
+       item < items; item += static_cast<int64_t>(gridDim.x) * kPer) {
+    const int slot = static_cast<int>(item / heads), h = static_cast<int>(item % heads);
+    const bool is_q = h < Hq;
+    const E* src = is_q ? q : k;
+    if (!src) continue;
+    const int64_t row = is_q ? static_cast<int64_t>(slot) * Hq + h
+                             : static_cast<int64_t>(slot) * Hkv + h - Hq;
+    typename P::Regs x;
+    part.load(x, src + row * kHeadDim);
+    const SeqMeta& M = meta[slot];
+    if (!M.active) continue;
+    SinCos sc[P::kPairs];
+    part.angles(sc, r, M.prompt_len + M.step);
+    part.rotate(x, sc);
+    part.store(x, (is_q ? q_out : k_out) + row * kHeadDim);
+  }
 }
 
 // Rows x [heads][rows][128] at positions first + j, or positions [heads][rows].  The heads
@@ -141,21 +147,24 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(RotaryLaunch r, c
                                                                const int32_t* positions,
                                                                int per) {
   using P = Part<E, ADJACENT, PACKED>;
-  const int j = blockIdx.x * (kThreads / P::kLanes) + threadIdx.x / P::kLanes;
-  if (j >= rows) return;
+  constexpr int kPer = kThreads / P::kLanes;
   const P part(threadIdx.x % P::kLanes, r.half);
   SinCos sc[P::kPairs];
-  if (!positions) part.angles(sc, r, first + j);
-  for (int64_t h0 = static_cast<int64_t>(blockIdx.y) * per; h0 < heads;
-       h0 += static_cast<int64_t>(gridDim.y) * per) {
-    const int64_t end = h0 + per < heads ? h0 + per : heads;
-    for (int64_t h = h0; h < end; ++h) {
-      const int64_t row = h * rows + j;
-      typename P::Regs v;
-      part.load(v, x + row * kHeadDim);
-      if (positions) part.angles(sc, r, positions[row]);
-      part.rotate(v, sc);
-      part.store(v, out + row * kHeadDim);
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * kPer + threadIdx.x / P::kLanes; at < rows;
+       at += static_cast<int64_t>(gridDim.x) * kPer) {
+    const int j = static_cast<int>(at);
+    if (!positions) part.angles(sc, r, first + j);
+    for (int64_t h0 = static_cast<int64_t>(blockIdx.y) * per; h0 < heads;
+         h0 += static_cast<int64_t>(gridDim.y) * per) {
+      const int64_t end = h0 + per < heads ? h0 + per : heads;
+      for (int64_t h = h0; h < end; ++h) {
+        const int64_t row = h * rows + j;
+        typename P::Regs v;
+        part.load(v, x + row * kHeadDim);
+        if (positions) part.angles(sc, r, positions[row]);
+        part.rotate(v, sc);
+        part.store(v, out + row * kHeadDim);
+      }
     }
   }
 }
@@ -180,7 +189,7 @@ void rotate_step(const SeqMeta* meta, int max_seqs, int Hq, int Hkv, const Rotar
     const int64_t threads =
         static_cast<int64_t>(max_seqs) * (Hq + Hkv) * Part<E, kAdjacent, kPacked>::kLanes;
     hipLaunchKernelGGL((rotate_step_kernel<E, kAdjacent, kPacked>),
-                       dim3(static_cast<unsigned>((threads + kThreads - 1) / kThreads)),
+                       dim3(workgroups((threads + kThreads - 1) / kThreads)),
                        dim3(kThreads), 0, s, meta, max_seqs, Hq, Hkv, r, static_cast<const E*>(q),
                        static_cast<const E*>(k), static_cast<E*>(q_out), static_cast<E*>(k_out));
   });
@@ -192,7 +201,7 @@ void rotate_rows(const RotaryLaunch& r, const void* x, void* out, int64_t heads,
   with_part<E>(r, [&](auto adjacent, auto packed) {
     constexpr bool kAdjacent = decltype(adjacent)::value, kPacked = decltype(packed)::value;
     const int tile = kThreads / Part<E, kAdjacent, kPacked>::kLanes;
-    const unsigned tiles = static_cast<unsigned>((static_cast<int64_t>(rows) + tile - 1) / tile);
+    const unsigned tiles = workgroups((static_cast<int64_t>(rows) + tile - 1) / tile);
     // heads to a workgroup: up to eight, which share their angles, while the workgroups are many
     // (50 fp32 heads of 2,113 rows, positions of their own: 8 heads 27 us)
     const int64_t all = heads * tiles / 4096;

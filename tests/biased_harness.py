@@ -25,14 +25,14 @@ def held(x, dtype):
 class Sim:
     def __init__(self, L, Hq, Hkv, K, lps, r=16, every=16, dtype=B.RA_BF16,
                  layout=B.RA_LAYOUT_CHRONOLOGICAL, weights=True, max_seqs=None, page_rows=32,
-                 seed=1, policy=B.RA_POLICY_RANDOM, extra_rows=0):
+                 seed=1, policy=B.RA_POLICY_RANDOM, extra_rows=0, attn_split=0):
         self.L, self.Hq, self.Hkv, self.G = L, Hq, Hkv, Hq // Hkv
         self.K, self.r, self.every, self.dtype = K, r, every, dtype
         self.n = max_seqs or len(lps)
         self.tdtype = torch.float32 if dtype == B.RA_F32 else torch.bfloat16
         self.gen = torch.Generator().manual_seed(seed)
         self.cfg = B.make_config(L, Hq, Hkv, K, r, every, dtype=dtype, max_seqs=self.n,
-                                 layout=layout, page_rows=page_rows, policy=policy,
+                                 layout=layout, page_rows=page_rows, policy=policy, attn_split=attn_split,
                                  max_prompt_len=max(lps, default=0))
         rows = sum(B.ra_seq_rows(self.cfg, lp) for lp in lps) + extra_rows
         self.cache = B.Cache(self.cfg, rows)

@@ -207,6 +207,44 @@ def test_a_rule_of_zeros_and_mixed_layers():
             sim.close()
 
 
+@pytest.mark.parametrize("order", ["plain first", "biased first", "alternate"])
+def test_layers_either_way_after_a_deferred_event(order):
+    """An event whose row moves are deferred, then a step of which some layers carry their moves
+    and others do not: every layer's rows move once."""
+    # (a head to a work item: such events defer their moves)
+    sim = Sim(4, 4, 2, 40, [30, 12], r=8, every=16, weights=False, attn_split=4096)
+    rule = B.make_score_rule()
+    calls = dict(zip(("plain first", "biased first", "alternate"),
+                     ([0, 0, 1, 1], [1, 1, 0, 0], [0, 1, 0, 1])))[order]
+    deferred = 0
+    for t in range(100):
+        pending = B.ra_get_seq_info(sim.h, 0).move_pending
+        deferred += pending
+        for l in range(4):
+            q, k, v = sim.inputs()
+            out = torch.empty(2, 4, 128, dtype=torch.bfloat16, device=DEV)
+            biased = pending and calls[l]
+            call = (lambda *a: sim.cache.decode_biased(l, rule, *a)) if biased else \
+                (lambda *a: sim.cache.decode(l, *a))
+            call(q.to(DEV), k.to(DEV), v.to(DEV), out)
+            for s in range(2):
+                sim.follow(s, l, q, k, v, out, {}, (t, order))
+        B.ra_end_step(sim.h)
+        for s, seq in sim.seq.items():
+            seq["step"] += 1
+            m = len(seq["heads"][0, 0]["P"]) - seq["lp"] - sim.r - sim.K
+            if seq["step"] % sim.every == 0 and m > 0:
+                pos = torch.empty(4, 2, B.ra_get_seq_info(sim.h, s).len, dtype=torch.int32, device=DEV)
+                B.ra_export_positions(sim.h, s, pos)      # (leaves the moves pending)
+                for (l, g), h in seq["heads"].items():
+                    keep = np.isin(h["P"], pos[l, g].cpu().numpy())
+                    for x in ("P", "K", "V", "W", "E"):
+                        h[x] = h[x][keep]
+    assert deferred >= 3
+    sim.check()
+    sim.close()
+
+
 def test_every_run_is_the_same():
     """Outputs and weights of two runs of the same steps, in splits, bit for bit."""
     got = []

@@ -112,12 +112,14 @@ def test_events_of_many_slots():
     sim.close()
 
 
+@pytest.mark.parametrize("dtype", [B.RA_BF16, B.RA_E4M3, B.RA_F32])
 @pytest.mark.parametrize("layout", [CHRON, PAGED])
-def test_fast_forward_and_resume(layout):
+def test_fast_forward_and_resume(layout, dtype):
     """A request preempted after events by weight resumes in another slot as it was: the same
     outputs, kept rows and weights as one that went on."""
     kw = dict(cap=10.0)
-    sim = Sim(2, 4, 2, 24, [20, 9], r=8, every=8, layout=layout, max_seqs=3, extra_rows=2 * 2 * 96)
+    sim = Sim(2, 4, 2, 24, [20, 9], r=8, every=8, dtype=dtype, layout=layout, max_seqs=3,
+              extra_rows=2 * 2 * 96)
     rule = sim.rule(kw)
     for t in range(43):
         sim.step(rule, kw, (t,))
