@@ -64,8 +64,14 @@ ra_status rotary_turns(const ra_rotary* p, ra::RotaryLaunch& out) {
   out.half = p->dims / 2;
   out.adjacent = p->pairs == RA_PAIRS_ADJACENT;
   out.magnitude = p->magnitude == 0.0 ? 1.f : static_cast<float>(p->magnitude);
+  // base^(-2i / dims) as a product of two powers: 16 of them, not 64 (a microsecond a call)
+  double high[8], low[8];
+  for (int i = 0; i < 8; ++i) {
+    high[i] = 8 * i < out.half ? std::pow(p->base, -16.0 * i / p->dims) : 0.0;
+    low[i] = i < out.half ? std::pow(p->base, -2.0 * i / p->dims) : 0.0;
+  }
   for (int i = 0; i < ra::kHeadDim / 2; ++i) {
-    const double f = std::pow(p->base, -2.0 * i / p->dims);
+    const double f = high[i / 8] * low[i % 8];
     double own = 1.0;    // share of the pair's own frequency, the rest divided by factor
     if (p->scaling == RA_ROTARY_LINEAR) {
       own = 0.0;

@@ -1224,16 +1224,20 @@ void launch_weighed(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpo
 hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpool, void* vpool,
                                 const int32_t* pos, float* weights, int slot_lo, int slot_hi,
                                 int max_candidates, hipStream_t s) {
-  // rows move down by less than a chunk: an event drops up to `every` rows, but under the
-  // external policy, whose rows pile up
+  // A workgroup to a chunk from the third chunk on (microseconds per event, selection
+  // included, by head and by chunk; bf16: 4 heads of 560 rows 26 and 33, 288 of them 53 and 55,
+  // 8 of 1,070 35 and 29, of 4,140 79 and 36, 64 of 4,140 115 and 75, 288 of 1,070 83 and 77, of
+  // 4,140 299 and 232, 2,304 of 4,140 1822 and 1739; fp32, half the rows to a chunk: 8 of 1,070
+  // 63 and 36, 288 of 4,140 652 and 457), but not for many e4m3 heads (288 of 4,140 159 and 144,
+  // 1,152 of 2,100 317 and 332, 2,304 of 4,140 1033 and 1116).  Rows have to move down by less
+  // than a chunk: an event drops up to `every` rows, but under the external policy.
   const int chunk = event_chunk_rows(sh.dtype);
   const int64_t n = (static_cast<int64_t>(max_candidates) + sh.r + 7 + chunk - 1) / chunk;
   const int64_t heads =
       static_cast<int64_t>(sh.due && sh.due->n ? sh.due->n : slot_hi - slot_lo) * sh.L * sh.Hkv;
-  const int n_chunks = sh.policy != 4 && sh.every + 8 <= chunk && n <= kMaxChunks &&
-                               heads * n <= (1 << 20)
-                           ? static_cast<int>(n)
-                           : 1;
+  const bool chunked = n > 2 && n <= kMaxChunks && heads * n <= (1 << 20) &&
+                       (sh.dtype != 2 || heads <= 512) && sh.policy != 4 && sh.every + 8 <= chunk;
+  const int n_chunks = chunked ? static_cast<int>(n) : 1;
   if (sh.dtype == 2)
     launch_weighed<uint8_t>(sh, meta, kpool, vpool, pos, weights, slot_lo, slot_hi, n_chunks, s);
   else if (sh.dtype == 1)

@@ -32,8 +32,9 @@ def _check(got, x, positions, freqs, adjacent, magnitude):
     """fp32: sine and cosine within 3 * 2^-23 of their own (the rounding of an angle of an
     eighth of a turn and the functions' error), times the magnitude (a rounding), two products
     and a sum (a rounding each): 8 * 2^-23 of |a| + |b|, then the output's half step.  The angle
-    itself is off by the fp64 roundings of the frequency, its turns and their product, here and
-    there: 2^-51 of it.  Channels that stay are equal."""
+    itself is off by fp64 roundings: here of two powers (half a step each, and their exponents'
+    2^-53 |ln f|, 14 at most, halved for each), their product, the turns and the angle, there
+    of one power, its angle and the remainder: under 2^-49 of it.  Channels that stay are equal."""
     dims = 2 * len(freqs)
     want = rotary.rotate(_f64(x), positions, freqs, adjacent, magnitude)
     got, x = _f64(got), _f64(x)
@@ -44,7 +45,7 @@ def _check(got, x, positions, freqs, adjacent, magnitude):
     size = magnitude * (np.abs(x[..., a]) + np.abs(x[..., b]))
     bound = np.zeros_like(x)
     angle = np.abs(np.asarray(positions, np.float64))[..., None] * freqs
-    bound[..., a] = bound[..., b] = (8 * 2.0 ** -23 + 2.0 ** -51 * angle) * size
+    bound[..., a] = bound[..., b] = (8 * 2.0 ** -23 + 2.0 ** -49 * angle) * size
     return want[..., :dims], got[..., :dims], bound[..., :dims]
 
 
