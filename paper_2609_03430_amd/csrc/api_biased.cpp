@@ -231,6 +231,7 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   b.window = rule->window;
   b.prefix = rule->prefix;
   b.ordered = ordered;
+  b.rows = static_cast<int>(std::min<int64_t>(int64_t(most) * ra::kBlockRows, INT32_MAX));
   ra::score_units(b);
   if (c->weights) {
     b.weights = c->weights;

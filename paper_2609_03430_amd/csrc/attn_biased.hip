@@ -5,8 +5,9 @@
 //   s = -inf where p_new - p_j >= window and p_j >= prefix
 // with p the cached positions, so the rule means the same before and after evictions.
 // A weight p_hj = exp(s_hj - m_h) / l_h needs the head's maximum and sum, which are known
-// after its last row: the attention stores the scores (G floats per row, 20 bytes beside
-// the 512 of a bf16 row at G = 5) and add_weights_kernel adds up the weights from them.
+// after its last row, so the scores are kept until then: in LDS where a workgroup takes a
+// whole head and they fit, else in the workspace (G floats per row, 20 bytes beside the 512 of
+// a bf16 row at G = 5), from which add_weights_kernel adds up the weights.
 #include "attn_rows.h"
 
 namespace ra {
@@ -51,8 +52,10 @@ struct BiasedSplits {
   __device__ __forceinline__ int operator()(const AttnLaunch&, int) const { return n; }
 };
 
-// The units of the scores; with KEEP each query's maximum and sum of a head, for
-// add_weights_kernel.
+// What becomes of the weights: not kept, added up by a launch of its own, or at once.
+constexpr int kNoWeights = 0, kWeighAfter = 1, kWeighHere = 2;
+
+// The units of the scores; with KEEP each query's maximum and sum of a head.
 template <bool KEEP>
 struct RuleEnds {
   static constexpr bool kKeeps = KEEP;
@@ -104,10 +107,41 @@ __device__ __forceinline__ void store16(__amdgpu_buffer_rsrc_t to, uint32_t offs
   __builtin_amdgcn_raw_buffer_store_b128(v, to, static_cast<int>(offset), 0, 0);
 }
 
+// w_j += sum over the group's queries of exp(s_j - m) / l for the four attended rows from
+// `at` on, the new row's weight set.  A row's sum is made by one thread, in the order of the
+// queries: the same on every run.  score4(q): their scores; stats [G][2].
+struct FourRows {
+  int64_t row;       // pool row of the first
+  int j;             // its index; past the cached rows: nothing to do
+};
+template <bool PAGED>
+__device__ __forceinline__ FourRows four_rows(const WindowBlocks& win, const RowMap& rm, int len,
+                                              int at) {
+  const int i = at / kBlockRows;
+  if (i >= win.n) return {0, len + 1};
+  const int j = (i < win.head ? i : i + win.shift) * kBlockRows + at % kBlockRows;
+  return {j > len ? 0 : pool_row<PAGED>(rm, j), j};
+}
+template <typename Score4>
+__device__ __forceinline__ void weigh_rows(f32x4* to, f32x4 w, int j, int len, int G,
+                                           const float* stats, float unit, Score4&& score4) {
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int q = 0; q < G; ++q) {
+    const f32x4 x = score4(q);
+    const float m = stats[2 * q], inv = 1.f / stats[2 * q + 1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += exp2_fast((x[e] - m) * unit) * inv;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = j + e < len ? w[e] + sum[e] : j + e == len ? sum[e] : w[e];
+  *to = w;
+}
+
 // The four wavefronts of a workgroup and their register buffers as in attn_blocks_kernel.
 // BYPOS: the rule has slopes or a window, and the positions are read with the rows (e4m3
 // rows then take up to 256 registers, two workgroups to a CU).
-template <typename R, int W, int MINW, bool PAGED, bool BYPOS, bool WEIGH>
+template <typename R, int W, int MINW, bool PAGED, bool BYPOS, int WEIGH>
 __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
     AttnLaunch a, BiasLaunch bias, SlotOrder order, Paging pg, uint8_t* k_scale, uint8_t* v_scale,
     int G, int Hq, int Hkv) {
@@ -117,6 +151,8 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   __shared__ float s_l[W][kMaxGroup];
   __shared__ __align__(16) float s_o[W][kMaxGroup][kHeadDim];
   __shared__ __align__(16) typename R::New s_new;
+  __shared__ float s_stats[WEIGH == kWeighHere ? kMaxGroup : 1][2];
+  extern __shared__ __align__(16) float s_scores[];      // WEIGH == kWeighHere: [G][lds_stride]
   const BiasedWork w = locate_biased(a, bias, order, Hkv, pg);
   if (!w.valid) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -212,7 +248,15 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
         for (int e = 0; e < 8; ++e)
           if (8 * grp + e >= limit) x[e] = kNegInf;
       }
-      if constexpr (WEIGH) {
+      if constexpr (WEIGH == kWeighHere) {
+        if (qi < G) {
+          f32x4* to = reinterpret_cast<f32x4*>(s_scores + qi * bias.lds_stride + kBlockRows * i +
+                                               8 * grp);
+          to[0] = f32x4{x[0], x[1], x[2], x[3]};
+          to[1] = f32x4{x[4], x[5], x[6], x[7]};
+        }
+      }
+      if constexpr (WEIGH == kWeighAfter) {
         // (lanes of no query write past the buffer's end, which drops them: a store that some
         // of them branched around would leave the loads in flight behind it uncounted)
         const uint32_t at = qi < G ? q_offset + 4u * (kBlockRows * G * i) : ~31u;
@@ -252,10 +296,33 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   }
   if constexpr (std::is_same_v<R, E4m3Rows>) R::gather_channels(st);
   const BiasedSplits splits{w.slot, w.nsplit};
-  RuleEnds<WEIGH> ends{bias.unit, nullptr};
-  if constexpr (WEIGH) ends.to = bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G);
+  // a whole head: its first rows' weights come while the wavefronts merge
+  const int first = static_cast<int>(threadIdx.x) * 4;
+  FourRows rows{0, 0};
+  f32x4 weights = {0.f, 0.f, 0.f, 0.f};
+  RuleEnds<WEIGH != kNoWeights> ends{bias.unit, nullptr};
+  if constexpr (WEIGH == kWeighAfter)
+    ends.to = bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G);
+  if constexpr (WEIGH == kWeighHere) {
+    ends.to = &s_stats[0][0];
+    rows = four_rows<PAGED>(w.win, w.rm, w.len, first);
+    if (rows.j <= w.len) weights = *reinterpret_cast<const f32x4*>(bias.weights + rows.row);
+  }
   finish_item<E, W, true, BiasedSplits, typename R::Channels>(
       a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits, ends);
+  if constexpr (WEIGH == kWeighHere) {
+    __syncthreads();
+    for (int at = first; at < w.win.n * kBlockRows;) {
+      if (rows.j <= w.len)
+        weigh_rows(reinterpret_cast<f32x4*>(bias.weights + rows.row), weights, rows.j, w.len, G,
+                   &s_stats[0][0], bias.unit, [&](int q) {
+                     return *reinterpret_cast<const f32x4*>(s_scores + q * bias.lds_stride + at);
+                   });
+      at += 4 * 64 * W;
+      rows = four_rows<PAGED>(w.win, w.rm, w.len, at);
+      if (rows.j <= w.len) weights = *reinterpret_cast<const f32x4*>(bias.weights + rows.row);
+    }
+  }
   if (owns_last) {
     const int64_t row = pool_row<PAGED>(w.rm, w.len);
     s_new.append(a, row, k_scale, v_scale);
@@ -263,9 +330,8 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   }
 }
 
-// w_j += sum over the group's queries of exp(s_j - m) / l, the new row's weight set.  A
-// row's sum is made by one thread, in the order of the queries: the same on every run.
-// Grid: (runs of 1,024 attended rows, KV heads, slots), four rows to a thread.
+// The weights of a launch whose scores went to the workspace.  Grid: (runs of 1,024 attended
+// rows, KV heads, slots), four rows to a thread.
 constexpr int kWeighThreads = 256, kWeighRows = 4;
 template <bool PAGED>
 __global__ __launch_bounds__(kWeighThreads) void add_weights_kernel(const SeqMeta* meta, int layer,
@@ -277,47 +343,38 @@ __global__ __launch_bounds__(kWeighThreads) void add_weights_kernel(const SeqMet
   const int len = M.len;
   const WindowBlocks win = window_blocks(len, bias.ordered ? bias.window : 0, bias.prefix);
   const int at = (blockIdx.x * kWeighThreads + threadIdx.x) * kWeighRows;
-  const int i = at / kBlockRows;
-  if (i >= win.n) return;
-  const int j = (i < win.head ? i : i + win.shift) * kBlockRows + at % kBlockRows;
-  if (j > len) return;
+  const FourRows rows = four_rows<PAGED>(win, row_map(M, slot, layer * Hkv + g, pg), len, at);
+  if (rows.j > len) return;
   const int64_t head = static_cast<int64_t>(slot) * Hq + g * G;
-  const float* s = bias.scores + head * bias.score_stride + static_cast<int64_t>(i) * G * kBlockRows +
-                   at % kBlockRows;
-  const float* st = bias.stats + 2 * head;
-  const RowMap rm = row_map(M, slot, layer * Hkv + g, pg);
-  f32x4* to = reinterpret_cast<f32x4*>(bias.weights + pool_row<PAGED>(rm, j));
-  f32x4 w = *to, sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int q = 0; q < G; ++q) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(s + q * kBlockRows);
-    const float m = st[2 * q], inv = 1.f / st[2 * q + 1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += exp2_fast((x[e] - m) * bias.unit) * inv;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = j + e < len ? w[e] + sum[e] : j + e == len ? sum[e] : w[e];
-  *to = w;
+  const float* s = bias.scores + head * bias.score_stride +
+                   static_cast<int64_t>(at / kBlockRows) * G * kBlockRows + at % kBlockRows;
+  f32x4* to = reinterpret_cast<f32x4*>(bias.weights + rows.row);
+  weigh_rows(to, *to, rows.j, len, G, bias.stats + 2 * head, bias.unit, [&](int q) {
+    return *reinterpret_cast<const f32x4*>(s + q * kBlockRows);
+  });
 }
 
-template <typename R, bool PAGED, bool BYPOS, bool WEIGH>
+template <typename R, bool PAGED, bool BYPOS, int WEIGH>
 void launch_biased(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hipStream_t s) {
   constexpr int kMinWaves = BYPOS && R::kWaves > 2 ? 2 : R::kWaves;
   const SlotOrder order = sh.order ? *sh.order : SlotOrder{};
   const dim3 grid(a.max_splits, sh.Hkv, order.n ? order.n : a.max_seqs);
-  hipLaunchKernelGGL((attn_biased_kernel<R, 4, kMinWaves, PAGED, BYPOS, WEIGH>), grid, dim3(256), 0,
-                     s, a, b, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
+  hipLaunchKernelGGL((attn_biased_kernel<R, 4, kMinWaves, PAGED, BYPOS, WEIGH>), grid, dim3(256),
+                     WEIGH == kWeighHere ? sh.G * b.lds_stride * sizeof(float) : 0, s, a, b, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
 }
 
 template <typename R, bool PAGED>
 void launch_rows(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hipStream_t s) {
   const bool by_position = b.slopes || b.window > 0;
-  if (b.weights) {
-    if (by_position) launch_biased<R, PAGED, true, true>(sh, a, b, s);
-    else launch_biased<R, PAGED, false, true>(sh, a, b, s);
+  if (!b.weights) {
+    if (by_position) launch_biased<R, PAGED, true, kNoWeights>(sh, a, b, s);
+    else launch_biased<R, PAGED, false, kNoWeights>(sh, a, b, s);
+  } else if (b.lds_stride) {
+    if (by_position) launch_biased<R, PAGED, true, kWeighHere>(sh, a, b, s);
+    else launch_biased<R, PAGED, false, kWeighHere>(sh, a, b, s);
   } else {
-    if (by_position) launch_biased<R, PAGED, true, false>(sh, a, b, s);
-    else launch_biased<R, PAGED, false, false>(sh, a, b, s);
+    if (by_position) launch_biased<R, PAGED, true, kWeighAfter>(sh, a, b, s);
+    else launch_biased<R, PAGED, false, kWeighAfter>(sh, a, b, s);
   }
 }
 
@@ -329,13 +386,23 @@ void launch_layout(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hi
 
 }  // namespace
 
-hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b,
+hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& given,
                                    hipStream_t s) {
+  BiasLaunch b = given;
+  // whole heads whose scores, beside 38 KB of LDS for the merge, leave a CU the workgroups that
+  // its registers do: three for e4m3 rows, two for bf16 (microseconds per layer in a captured
+  // step, weights after and at once: bf16, 2 heads of 200 rows 9.6 and 7.8, 128 of 700 18.2 and
+  // 16.0, 256 of 900 33.1 and 27.5, 512 of 1,100 73.0 and 64.7; e4m3, 8 of 300 10.0 and 8.5, 256
+  // of 200 13.3 and 10.9; fp32, 256 of 900 63.5 and 55.3)
+  const int64_t stride = b.rows + 4;       // (the queries' rows start in different banks)
+  const int64_t bytes = sh.G * stride * static_cast<int64_t>(sizeof(float));
+  if (b.weights && a.max_splits == 1 && bytes <= (sh.dtype == 2 ? 15 : 24) * 1024)
+    b.lds_stride = static_cast<int>(stride);
   if (sh.dtype == 2) launch_layout<E4m3Rows>(sh, a, b, s);
   else if (sh.dtype == 1) launch_layout<Bf16Rows>(sh, a, b, s);
   else launch_layout<F32Rows>(sh, a, b, s);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !b.weights) return e;
+  if (e != hipSuccess || !b.weights || b.lds_stride) return e;
   const int rows = a.max_splits * a.split_keys;
   const int per = kWeighThreads * kWeighRows;
   const dim3 grid((rows + per - 1) / per, sh.Hkv, a.max_seqs);

@@ -327,6 +327,8 @@ struct BiasLaunch {
   float* scores = nullptr;
   int64_t score_stride = 0;
   float* stats = nullptr;
+  int rows = 0;                   // attended rows of the longest head, in whole blocks
+  int lds_stride = 0;             // set by the launch: the scores stay in LDS, rows apart
 };
 // Scores stay as the products (or tanh of them) give them until a difference is taken, so
 // that no rounding of a score of 40 weighs in its exponential; slopes take them in natural

@@ -91,6 +91,20 @@ def test_long_heads_in_splits(dtype, G):
         sim.close()
 
 
+@pytest.mark.parametrize("dtype,layout", [(B.RA_BF16, CHRON), (B.RA_E4M3, PAGED), (B.RA_F32, PAGED)])
+def test_weights_of_many_whole_heads(dtype, layout):
+    """132 heads, a workgroup each, whose scores stay in LDS and take two rounds of rows; ragged
+    ones; a window's two runs of blocks."""
+    for lens, kw in (([1300] * 33, {}), ([1 + 37 * i for i in range(33)], dict(window=700, prefix=40)),
+                     ([1290 - i for i in range(33)], dict(window=1200, prefix=3, cap=9.0))):
+        sim = Sim(1, 8, 4, 0, lens, r=0, every=64, dtype=dtype, layout=layout)
+        rule = sim.rule(kw)
+        for t in range(2):
+            sim.step(rule, kw, (t,))
+        sim.check()
+        sim.close()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_one_head_of_more_rows_than_its_splits_hold_at_512(dtype):
     """One head of 33,000 rows (65 splits of 512) and a short one beside it."""
