@@ -232,6 +232,7 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   b.prefix = rule->prefix;
   b.ordered = ordered;
   b.rows = static_cast<int>(std::min<int64_t>(int64_t(most) * ra::kBlockRows, INT32_MAX));
+  b.heads = n_active * c->cfg.num_kv_heads;
   ra::score_units(b);
   if (c->weights) {
     b.weights = c->weights;

@@ -389,14 +389,16 @@ void launch_layout(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hi
 hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& given,
                                    hipStream_t s) {
   BiasLaunch b = given;
-  // whole heads whose scores, beside 38 KB of LDS for the merge, leave a CU the workgroups that
-  // its registers do: three for e4m3 rows, two for bf16 (microseconds per layer in a captured
-  // step, weights after and at once: bf16, 2 heads of 200 rows 9.6 and 7.8, 128 of 700 18.2 and
-  // 16.0, 256 of 900 33.1 and 27.5, 512 of 1,100 73.0 and 64.7; e4m3, 8 of 300 10.0 and 8.5, 256
-  // of 200 13.3 and 10.9; fp32, 256 of 900 63.5 and 55.3)
+  // whole heads whose scores fit a CU's 160 KB beside the 38 KB of the merge: of one workgroup
+  // where there are no more heads than CUs, or of as many as its registers hold, one for fp32
+  // rows, two for bf16, three for e4m3 (microseconds per layer in a captured step, weights
+  // after and at once: bf16, 2 heads of 200 rows 9.6 and 7.8, 128 of 700 18.2 and 16.0, 256 of
+  // 900 33.1 and 27.5, 512 of 1,100 73.0 and 64.7; e4m3, 8 of 300 10.0 and 8.5, 256 of 200 13.3
+  // and 10.9; fp32, 256 of 900 63.5 and 55.3)
+  const bool alone = sh.dtype == 0 || b.heads <= 256;
   const int64_t stride = b.rows + 4;       // (the queries' rows start in different banks)
   const int64_t bytes = sh.G * stride * static_cast<int64_t>(sizeof(float));
-  if (b.weights && a.max_splits == 1 && bytes <= (sh.dtype == 2 ? 15 : 24) * 1024)
+  if (b.weights && a.max_splits == 1 && bytes <= (alone ? 118 : sh.dtype == 2 ? 15 : 24) * 1024)
     b.lds_stride = static_cast<int>(stride);
   if (sh.dtype == 2) launch_layout<E4m3Rows>(sh, a, b, s);
   else if (sh.dtype == 1) launch_layout<Bf16Rows>(sh, a, b, s);

@@ -328,6 +328,7 @@ struct BiasLaunch {
   int64_t score_stride = 0;
   float* stats = nullptr;
   int rows = 0;                   // attended rows of the longest head, in whole blocks
+  int heads = 0;                  // heads of the active slots
   int lds_stride = 0;             // set by the launch: the scores stay in LDS, rows apart
 };
 // Scores stay as the products (or tanh of them) give them until a difference is taken, so
