@@ -6,8 +6,8 @@
 // with p the cached positions, so the rule means the same before and after evictions.
 // A weight p_hj = exp(s_hj - m_h) / l_h needs the head's maximum and sum, which are known
 // after its last row, so the scores are kept until then: in LDS where a workgroup takes a
-// whole head and they fit, else in the workspace (G floats per row, 20 bytes beside the 512 of
-// a bf16 row at G = 5), from which add_weights_kernel adds up the weights.
+// whole head, as many as fit, else in the workspace (G floats per row, 20 bytes beside the 512
+// of a bf16 row at G = 5).  Those of a head in splits are added up by add_weights_kernel.
 #include "attn_rows.h"
 
 namespace ra {
@@ -52,8 +52,9 @@ struct BiasedSplits {
   __device__ __forceinline__ int operator()(const AttnLaunch&, int) const { return n; }
 };
 
-// What becomes of the weights: not kept, added up by a launch of its own, or at once.
-constexpr int kNoWeights = 0, kWeighAfter = 1, kWeighHere = 2;
+// What becomes of the weights: not kept, added up by a launch of its own, or at once, from
+// scores in LDS or in LDS and the workspace both.
+constexpr int kNoWeights = 0, kWeighAfter = 1, kWeighHere = 2, kWeighBoth = 3;
 
 // The units of the scores; with KEEP each query's maximum and sum of a head.
 template <bool KEEP>
@@ -151,8 +152,10 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   __shared__ float s_l[W][kMaxGroup];
   __shared__ __align__(16) float s_o[W][kMaxGroup][kHeadDim];
   __shared__ __align__(16) typename R::New s_new;
-  __shared__ float s_stats[WEIGH == kWeighHere ? kMaxGroup : 1][2];
-  extern __shared__ __align__(16) float s_scores[];      // WEIGH == kWeighHere: [G][lds_stride]
+  constexpr bool kHere = WEIGH >= kWeighHere;
+  __shared__ float s_stats[kHere ? kMaxGroup : 1][2];
+  // kHere: [G][lds_stride], of each wavefront's blocks the first lds_blocks
+  extern __shared__ __align__(16) float s_scores[];
   const BiasedWork w = locate_biased(a, bias, order, Hkv, pg);
   if (!w.valid) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -248,18 +251,19 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
         for (int e = 0; e < 8; ++e)
           if (8 * grp + e >= limit) x[e] = kNegInf;
       }
-      if constexpr (WEIGH == kWeighHere) {
-        if (qi < G) {
-          f32x4* to = reinterpret_cast<f32x4*>(s_scores + qi * bias.lds_stride + kBlockRows * i +
-                                               8 * grp);
+      const bool in_lds = WEIGH == kWeighHere || (WEIGH == kWeighBoth && i - b0 < bias.lds_blocks);
+      if constexpr (kHere) {
+        if (in_lds && qi < G) {
+          const int at = kBlockRows * (wave * bias.lds_blocks + i - b0) + 8 * grp;
+          f32x4* to = reinterpret_cast<f32x4*>(s_scores + qi * bias.lds_stride + at);
           to[0] = f32x4{x[0], x[1], x[2], x[3]};
           to[1] = f32x4{x[4], x[5], x[6], x[7]};
         }
       }
-      if constexpr (WEIGH == kWeighAfter) {
+      if constexpr (WEIGH == kWeighAfter || WEIGH == kWeighBoth) {
         // (lanes of no query write past the buffer's end, which drops them: a store that some
         // of them branched around would leave the loads in flight behind it uncounted)
-        const uint32_t at = qi < G ? q_offset + 4u * (kBlockRows * G * i) : ~31u;
+        const uint32_t at = qi < G && !in_lds ? q_offset + 4u * (kBlockRows * G * i) : ~31u;
         store16(scores, at, x[0], x[1], x[2], x[3]);
         store16(scores, at + 16u, x[4], x[5], x[6], x[7]);
       }
@@ -303,21 +307,30 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   RuleEnds<WEIGH != kNoWeights> ends{bias.unit, nullptr};
   if constexpr (WEIGH == kWeighAfter)
     ends.to = bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G);
-  if constexpr (WEIGH == kWeighHere) {
+  if constexpr (kHere) {
     ends.to = &s_stats[0][0];
     rows = four_rows<PAGED>(w.win, w.rm, w.len, first);
     if (rows.j <= w.len) weights = *reinterpret_cast<const f32x4*>(bias.weights + rows.row);
   }
   finish_item<E, W, true, BiasedSplits, typename R::Channels>(
       a, w, wave, qi, grp, st, G, Hq, Hkv, s_m, s_l, s_o, splits, ends);
-  if constexpr (WEIGH == kWeighHere) {
+  if constexpr (kHere) {
+    // (a barrier after which the workgroup's own stores are there to read, too)
     __syncthreads();
+    const float* far = bias.scores + (static_cast<int64_t>(w.slot) * Hq + w.g * G) * bias.score_stride;
     for (int at = first; at < w.win.n * kBlockRows;) {
-      if (rows.j <= w.len)
+      if (rows.j <= w.len) {
+        const int i = at / kBlockRows, in_block = at % kBlockRows, owner = i / per;
+        const bool in_lds = WEIGH == kWeighHere || i - owner * per < bias.lds_blocks;
+        const float* near =
+            s_scores + kBlockRows * (owner * bias.lds_blocks + i - owner * per) + in_block;
+        const float* from = far + static_cast<int64_t>(i) * G * kBlockRows + in_block;
         weigh_rows(reinterpret_cast<f32x4*>(bias.weights + rows.row), weights, rows.j, w.len, G,
                    &s_stats[0][0], bias.unit, [&](int q) {
-                     return *reinterpret_cast<const f32x4*>(s_scores + q * bias.lds_stride + at);
+                     if (in_lds) return *reinterpret_cast<const f32x4*>(near + q * bias.lds_stride);
+                     return *reinterpret_cast<const f32x4*>(from + q * kBlockRows);
                    });
+      }
       at += 4 * 64 * W;
       rows = four_rows<PAGED>(w.win, w.rm, w.len, at);
       if (rows.j <= w.len) weights = *reinterpret_cast<const f32x4*>(bias.weights + rows.row);
@@ -360,7 +373,7 @@ void launch_biased(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hi
   const SlotOrder order = sh.order ? *sh.order : SlotOrder{};
   const dim3 grid(a.max_splits, sh.Hkv, order.n ? order.n : a.max_seqs);
   hipLaunchKernelGGL((attn_biased_kernel<R, 4, kMinWaves, PAGED, BYPOS, WEIGH>), grid, dim3(256),
-                     WEIGH == kWeighHere ? sh.G * b.lds_stride * sizeof(float) : 0, s, a, b, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
+                     WEIGH >= kWeighHere ? sh.G * b.lds_stride * sizeof(float) : 0, s, a, b, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
 }
 
 template <typename R, bool PAGED>
@@ -369,9 +382,12 @@ void launch_rows(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hipS
   if (!b.weights) {
     if (by_position) launch_biased<R, PAGED, true, kNoWeights>(sh, a, b, s);
     else launch_biased<R, PAGED, false, kNoWeights>(sh, a, b, s);
-  } else if (b.lds_stride) {
+  } else if (b.lds_stride && 4 * kBlockRows * b.lds_blocks >= b.rows) {
     if (by_position) launch_biased<R, PAGED, true, kWeighHere>(sh, a, b, s);
     else launch_biased<R, PAGED, false, kWeighHere>(sh, a, b, s);
+  } else if (b.lds_stride) {
+    if (by_position) launch_biased<R, PAGED, true, kWeighBoth>(sh, a, b, s);
+    else launch_biased<R, PAGED, false, kWeighBoth>(sh, a, b, s);
   } else {
     if (by_position) launch_biased<R, PAGED, true, kWeighAfter>(sh, a, b, s);
     else launch_biased<R, PAGED, false, kWeighAfter>(sh, a, b, s);
@@ -389,17 +405,24 @@ void launch_layout(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hi
 hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const BiasLaunch& given,
                                    hipStream_t s) {
   BiasLaunch b = given;
-  // whole heads whose scores fit a CU's 160 KB beside the 38 KB of the merge: of one workgroup
+  // whole heads keep what fits of a CU's 160 KB beside the 38 KB of the merge: of one workgroup
   // where there are no more heads than CUs, or of as many as its registers hold, one for fp32
-  // rows, two for bf16, three for e4m3 (microseconds per layer in a captured step, weights
-  // after and at once: bf16, 2 heads of 200 rows 9.6 and 7.8, 128 of 700 18.2 and 16.0, 256 of
-  // 900 33.1 and 27.5, 512 of 1,100 73.0 and 64.7; e4m3, 8 of 300 10.0 and 8.5, 256 of 200 13.3
-  // and 10.9; fp32, 256 of 900 63.5 and 55.3)
+  // rows, two for bf16, three for e4m3, where that is all of them (microseconds per layer in a
+  // captured step, weights after and at once: bf16, 2 heads of 200 rows 9.6 and 7.8, 128 of 700
+  // 18.2 and 16.0, 256 of 900 33.1 and 27.5, of 4,000 120 and 100, 512 of 1,100 73.0 and 64.7;
+  // e4m3, 8 of 300 10.0 and 8.5, 256 of 200 13.3 and 10.9, of 7,400 119 and 104; fp32, 256 of
+  // 900 63.5 and 55.3); part of them, the rest through the workspace, gain less (256 of 9,216, G
+  // = 5, 260 and 234, of 12,000, G = 8, 357 and 348), and under half of 16 queries' nothing (160
+  // e4m3 heads of 6,000 88 and 96)
   const bool alone = sh.dtype == 0 || b.heads <= 256;
-  const int64_t stride = b.rows + 4;       // (the queries' rows start in different banks)
-  const int64_t bytes = sh.G * stride * static_cast<int64_t>(sizeof(float));
-  if (b.weights && a.max_splits == 1 && bytes <= (alone ? 118 : sh.dtype == 2 ? 15 : 24) * 1024)
-    b.lds_stride = static_cast<int>(stride);
+  const int64_t room = (alone ? 118 : sh.dtype == 2 ? 15 : 24) * 256 / sh.G;   // floats a query
+  const int blocks = b.rows / kBlockRows, per_wave = (blocks + 3) / 4;
+  const int fit = static_cast<int>((room - 4) / (4 * kBlockRows));
+  if (b.weights && a.max_splits == 1 && fit > 0 &&
+      (per_wave <= fit || (alone && (sh.G <= 8 || per_wave <= 2 * fit)))) {
+    b.lds_blocks = per_wave < fit ? per_wave : fit;
+    b.lds_stride = 4 * kBlockRows * b.lds_blocks + 4;   // (queries start in different banks)
+  }
   if (sh.dtype == 2) launch_layout<E4m3Rows>(sh, a, b, s);
   else if (sh.dtype == 1) launch_layout<Bf16Rows>(sh, a, b, s);
   else launch_layout<F32Rows>(sh, a, b, s);

@@ -329,7 +329,8 @@ struct BiasLaunch {
   float* stats = nullptr;
   int rows = 0;                   // attended rows of the longest head, in whole blocks
   int heads = 0;                  // heads of the active slots
-  int lds_stride = 0;             // set by the launch: the scores stay in LDS, rows apart
+  int lds_blocks = 0;             // set by the launch: blocks of each wavefront whose scores
+  int lds_stride = 0;             //   stay in LDS, and the floats a query takes there
 };
 // Scores stay as the products (or tanh of them) give them until a difference is taken, so
 // that no rounding of a score of 40 weighs in its exponential; slopes take them in natural

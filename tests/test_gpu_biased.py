@@ -105,6 +105,21 @@ def test_weights_of_many_whole_heads(dtype, layout):
         sim.close()
 
 
+@pytest.mark.parametrize("dtype,layout", [(B.RA_BF16, PAGED), (B.RA_E4M3, CHRON), (B.RA_F32, CHRON)])
+def test_weights_of_whole_heads_longer_than_lds(dtype, layout):
+    """Scores of G = 16 and 2,000 rows (LDS holds 1,792), part of them in LDS and part in the
+    workspace; shorter heads of the same launch, all of whose are in LDS."""
+    lens = [2000] + [1999] * 4 + [1700, 1, 40, 1900] * 2
+    # (attn_split keeps the few heads whole)
+    sim = Sim(1, 16, 1, 0, lens, r=0, every=64, dtype=dtype, layout=layout, attn_split=4096)
+    kw = dict(cap=9.0, window=1800, prefix=100)
+    rule = sim.rule(kw)
+    for t in range(2):
+        sim.step(rule, kw, (t,))
+    sim.check()
+    sim.close()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_one_head_of_more_rows_than_its_splits_hold_at_512(dtype):
     """One head of 33,000 rows (65 splits of 512) and a short one beside it."""
