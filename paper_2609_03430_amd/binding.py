@@ -572,7 +572,7 @@ def ra_rotate_rows(rotary, x, out, first=0, positions=None, stream=None):
     one per row of x."""
     where = "ra_rotate_rows"
     _arg(x, where, "x")
-    if x.dtype not in (torch.float32, torch.bfloat16) or x.dim() < 2 or x.shape[-1] != 128:
+    if x is None or x.dtype not in (torch.float32, torch.bfloat16) or x.dim() < 2 or x.shape[-1] != 128:
         raise RandAttnError(RA_ERR_INVALID_ARG, where + " (x: not fp32 or bf16 rows of 128)")
     rows = x.shape[-2]
     n = x.numel() // 128

@@ -293,6 +293,48 @@ def test_every_run_is_the_same():
     assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+def test_rows_past_32_bits_of_elements():
+    """A request of 17 million rows, and one whose rows lie behind them: offsets past 2^31
+    elements of the pools, a window of the long one, its weights' sum."""
+    long, n = 17_000_000, 300
+    cfg = B.make_config(1, 2, 1, 8, 0, 8, max_seqs=2)
+    c = B.Cache(cfg, B.ra_required_slots(cfg, [long, n]))
+    c.attach_weights(long)
+    g = torch.Generator().manual_seed(8)
+    k, v = (torch.randn(1, 1, n, 128, generator=g).to(torch.bfloat16) for _ in range(2))
+    B.ra_seq_begin(c.handle, 0, long, 1, 0)              # (its rows are the pool's zeros)
+    B.ra_seq_begin(c.handle, 1, n, 1, 1, k.to(DEV), v.to(DEV))
+    assert B.ra_get_seq_info(c.handle, 1).base * 128 > 2 ** 31
+    K, V, W = _f64(k[0, 0]), _f64(v[0, 0]), np.zeros(n + 2)
+    for t, kw in enumerate((dict(), dict(window=100, prefix=7))):
+        q, kn, vn = (torch.randn(2, h, 128, generator=g).to(torch.bfloat16) for h in (2, 1, 1))
+        q[0], vn[0] = 0.0, 1.0                           # equal scores: 1 / rows in sight
+        out = torch.empty(2, 2, 128, dtype=torch.bfloat16, device=DEV)
+        c.decode_biased(0, B.make_score_rule(**kw), q.to(DEV), kn.to(DEV), vn.to(DEV), out)
+        B.ra_end_step(c.handle)
+        seen = 107 if kw else long + 1
+        # one row (the first step's pair is in sight of the second, too) of value 1
+        want = (2 if kw else 1) / seen
+        assert np.abs(_f64(out[0]) - want).max() <= 2.0 ** -8 * want + 2.0 ** -14 * want
+        K, V = np.vstack([K, _f64(kn[1])]), np.vstack([V, _f64(vn[1])])
+        for h in range(2):
+            want, p = rule_attention(_f64(q[1, h]), K, V, np.arange(len(K)), n + t, **kw)
+            assert (np.abs(_f64(out[1, h]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-4).all()
+            W[:len(p)] += p
+    w = torch.empty(1, 1, n + 2, device=DEV)
+    B.ra_export_weights(c.handle, 1, w)
+    # (scores of about 10 from 131 roundings each: 10^-4 of a weight of at most 1)
+    assert np.abs(_f64(w[0, 0]) - W).max() <= 1e-4
+    w = torch.empty(1, 1, long + 2, device=DEV)
+    B.ra_export_weights(c.handle, 0, w)
+    # each weight is 1 / (17 million + 1) and two of 1 / 107 in sight, to a few fp32 roundings
+    w = w[0, 0].double()
+    assert abs(float(w.sum()) - 4.0) <= 4 * 2.0 ** -18
+    assert abs(float(w[5_000_000]) * (long + 1) / 2 - 1) <= 2.0 ** -18
+    assert abs(float(w[3]) * 107 / 2 - 1) <= 2.0 ** -12
+    c.close()
+
+
 def test_more_slots_than_an_order_holds_and_other_streams():
     """300 ragged slots, steps on two streams in turn."""
     n = 300
