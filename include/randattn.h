@@ -565,7 +565,8 @@ ra_status ra_biased_attention(ra_cache* cache, int32_t layer, const ra_score_rul
  * one whose layout has no weights. */
 size_t ra_weights_bytes(const ra_config* cfg, int64_t pool_rows);
 
-/* Bytes of ra_biased_attention's workspace with weights attached, for prompts of up to
+/* Bytes of ra_biased_attention's workspace with weights attached (whose regions hold up to
+ * 2^25 rows a head: RA_ERR_UNSUPPORTED beyond), for prompts of up to
  * max_prompt_len rows (the paged layout: the config's max_prompt_len): the split partials and
  * num_q_heads floats per row.  0 as above, or if such a prompt does not fit the budget. */
 size_t ra_weights_workspace_bytes(const ra_config* cfg, int32_t max_prompt_len);

@@ -105,7 +105,7 @@ __global__ __launch_bounds__(NT) void weight_event_kernel(const SeqMeta* __restr
     }
   }
   // the r most recent rows follow, NT at a time: their sources lie above every row
-  // written so far, and those of later rounds above this round's destinations
+  // written so far, and those of later turns above the destinations of this one
   for (int j0 = lp + C; j0 < old_len; j0 += NT) {
     const int j = j0 + t;
     int32_t pj = 0;
