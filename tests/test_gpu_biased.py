@@ -371,12 +371,13 @@ def test_more_slots_than_an_order_holds_and_other_streams():
     c.close()
 
 
-def test_captured_steps():
-    """Steps captured once and replayed through events: outputs, kept sets and weights are an
-    eager twin's, bit for bit."""
-    kw = dict(cap=8.0, slopes=slopes(6), window=60, prefix=4)
+@pytest.mark.parametrize("lps,window", [([30, 3], 60), ([900, 90], 0)])
+def test_captured_steps(lps, window):
+    """Steps captured once and replayed through events, weights added at once or (heads in
+    splits) after: outputs, kept sets and weights are an eager twin's."""
+    kw = dict(cap=8.0, slopes=slopes(6), window=window, prefix=4)
     for dtype in DTYPES:
-        sims = [Sim(2, 6, 2, 40, [30, 3], r=8, every=8, dtype=dtype, seed=6) for _ in range(2)]
+        sims = [Sim(2, 6, 2, 40, lps, r=8, every=8, dtype=dtype, seed=6) for _ in range(2)]
         rules = [sim.rule(kw) for sim in sims]
         ins = [[x.to(DEV) for x in sims[0].inputs()] for _ in range(2)]
         outs = [torch.empty(2, 2, 6, 128, dtype=sims[0].tdtype, device=DEV) for _ in range(2)]
