@@ -89,10 +89,12 @@ ra_status rotary_turns(const ra_rotary* p, ra::RotaryLaunch& out) {
 
 // plan_blocks, but for two kinds of launches (microseconds per layer in a captured step,
 // plan_blocks and this):
-//   few fp32 rows, twice as long as those it was measured with: 64 keys to a workgroup while
-//     there is a CU for each, and no more than 512 (2 heads of 200 rows 13.3 and 10.5, of 500
-//     15.0 and 11.9; 8 heads of 600 17.4 and 13.8, of 9,000 35.0 and 30.3; but 64 heads of
-//     600, 640 workgroups, 20.4 and 35.3; 8 of 2,200 stay at 19.5, with 64 keys 26.5);
+//   few fp32 rows, twice as long as those it was measured with: 64 keys to a workgroup up to
+//     1,300 keys, for up to 16 heads 160 beyond, while there is a CU for each, and no more than
+//     512 (2 heads of 200 rows 13.3 and 10.5, of 500 15.0 and 11.9, of 5,000 25.6 and 21.8; 8
+//     heads of 600 17.4 and 13.8, of 1,200 18.5 and 16.4, of 2,200 19.6 and 18.2, with 64 keys
+//     26.5, of 5,000 26.1 and 22.0, of 9,000 35.0 and 30.3; but 64 heads of 600, 640 workgroups,
+//     20.4 and 35.3, 32 of 1,000 19.6 and, with 128 keys, 30.3);
 //   129 to 256 ragged heads, of which it makes one item each: six, so that the CUs of the short
 //     ones share the long ones' work (bf16, 160 heads of 300 to 9,000 rows 199 and 95, 256 of
 //     them 217 and 142, 192 of 4,500 to 9,000 226 and 148, of 200 to 3,000 69 and 43; e4m3, 192
@@ -102,8 +104,11 @@ Plan biased_plan(const ra_cache* c, int64_t keys_max, int64_t keys_mean, int hea
   if (c->cfg.attn_split > 0) return p;
   const auto items = [&](int64_t keys) { return (keys_max + keys - 1) / keys; };
   int64_t keys = p.split_keys;
-  if (c->cfg.dtype == RA_F32 && keys_max <= 1000 && items(64) * heads <= 256)
+  if (c->cfg.dtype == RA_F32 && keys_max <= 1300 && items(64) * heads <= 256)
     keys = 64;
+  else if (c->cfg.dtype == RA_F32 && heads <= 16 && items(160) * heads <= 256 &&
+           items(160) <= ra::kMaxSplits)
+    keys = 160;
   else if (c->cfg.dtype == RA_F32 && items(512) * heads <= 256 && items(512) <= ra::kMaxSplits)
     keys = std::min<int64_t>(keys, 512);
   else if (heads > 128 && heads <= 256 && keys_max >= 1536 && 8 * keys_mean < 7 * keys_max)
