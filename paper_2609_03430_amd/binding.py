@@ -263,6 +263,23 @@ def _torch_stream(handle, device):
             else torch.cuda.default_stream(device))
 
 
+# The weights tensor attached to every live handle that has one, and the streams of the calls
+# that have used it.  Each is told to the allocator once, which keeps the memory, when it is
+# given back, until the work on them has ended: the kernels of an event wait on words in it.
+_WEIGHTS = {}
+
+
+def _weights_stream(handle, stream):
+    """The raw stream of a call that uses the weights where any are attached."""
+    raw = _stream(stream)
+    if _WEIGHTS:
+        weights, streams = _WEIGHTS.get(getattr(handle, "value", handle), (None, None))
+        if weights is not None and raw not in streams:
+            weights.record_stream(_torch_stream(raw, weights.device))
+            streams.add(raw)
+    return raw
+
+
 def make_config(num_layers, num_q_heads, num_kv_heads, budget_k, recent_r=64,
                 evict_every=64, budget_mode=RA_BUDGET_EVICTABLE, dtype=RA_BF16,
                 max_seqs=1, head_dim=128, attn_split=0,
@@ -343,6 +360,7 @@ def ra_cache_create(cfg, k_pool, v_pool, pos_pool, pool_rows, meta, stream=None)
 def ra_cache_destroy(handle):
     _check(_lib().ra_cache_destroy(handle), "ra_cache_destroy")
     _CONFIGS.pop(getattr(handle, "value", handle), None)
+    _WEIGHTS.pop(getattr(handle, "value", handle), None)
 
 
 def ra_pool_info(handle):
@@ -362,7 +380,7 @@ def ra_seq_begin(handle, seq, prompt_len, seed, request_id, k_prompt=None,
         _arg(v_prompt, "ra_seq_begin", "v_prompt", _cache_dtype(cfg), n)
     _check(_lib().ra_seq_begin(handle, int(seq), int(prompt_len), int(seed),
                                int(request_id), _ptr(k_prompt), _ptr(v_prompt),
-                               _stream(stream)), "ra_seq_begin")
+                               _weights_stream(handle, stream)), "ra_seq_begin")
 
 
 def ra_seq_end(handle, seq, stream=None):
@@ -408,7 +426,7 @@ def ra_decode_attention_noalloc(handle, layer, q, k_new, v_new, out, stream=None
 
 def ra_end_step(handle, stream=None):
     n = ctypes.c_int32(0)
-    _check(_lib().ra_end_step(handle, _stream(stream), ctypes.byref(n)),
+    _check(_lib().ra_end_step(handle, _weights_stream(handle, stream), ctypes.byref(n)),
            "ra_end_step")
     return n.value
 
@@ -418,16 +436,17 @@ def ra_graph_mode(handle, on, stream=None):
 
 
 def ra_evict_now(handle, seq, stream=None):
-    _check(_lib().ra_evict_now(handle, int(seq), _stream(stream)), "ra_evict_now")
+    _check(_lib().ra_evict_now(handle, int(seq), _weights_stream(handle, stream)), "ra_evict_now")
 
 
 def ra_fast_forward(handle, n_steps, stream=None):
-    _check(_lib().ra_fast_forward(handle, int(n_steps), _stream(stream)),
+    _check(_lib().ra_fast_forward(handle, int(n_steps), _weights_stream(handle, stream)),
            "ra_fast_forward")
 
 
 def ra_seq_fast_forward(handle, seq, n_steps, stream=None):
-    _check(_lib().ra_seq_fast_forward(handle, int(seq), int(n_steps), _stream(stream)),
+    _check(_lib().ra_seq_fast_forward(handle, int(seq), int(n_steps),
+                                      _weights_stream(handle, stream)),
            "ra_seq_fast_forward")
 
 
@@ -597,7 +616,7 @@ def ra_biased_attention(handle, layer, rule, q, k_new, v_new, out, workspace, st
     _check(_lib().ra_biased_attention(handle, int(layer), ctypes.byref(rule), _ptr(q), _ptr(k_new),
                                       _ptr(v_new), _ptr(out), _ptr(workspace),
                                       0 if workspace is None else _bytes(workspace),
-                                      _stream(stream)), where)
+                                      _weights_stream(handle, stream)), where)
 
 
 def ra_weights_bytes(cfg, pool_rows):
@@ -609,12 +628,18 @@ def ra_weights_workspace_bytes(cfg, max_prompt_len):
 
 
 def ra_weights_attach(handle, weights):
-    """Attach a weights buffer (an fp32 device tensor kept alive by the caller), or detach
-    with None."""
+    """Attach a weights buffer (an fp32 device tensor, kept until another is attached, None or
+    the handle's end, and its memory until the calls made with it have ended, whatever their
+    streams), or detach with None."""
     _arg(weights, "ra_weights_attach", "weights", torch.float32)
     _check(_lib().ra_weights_attach(handle, _ptr(weights),
                                     0 if weights is None else _bytes(weights)),
            "ra_weights_attach")
+    key = getattr(handle, "value", handle)
+    if weights is None:
+        _WEIGHTS.pop(key, None)
+    else:
+        _WEIGHTS[key] = (weights, set())
 
 
 def _row_values(handle, seq):
@@ -626,14 +651,15 @@ def _row_values(handle, seq):
 def ra_write_weights(handle, seq, weights, stream=None):
     where = "ra_write_weights"
     _arg(weights, where, "weights", torch.float32, _row_values(handle, seq))
-    _check(_lib().ra_write_weights(handle, int(seq), _ptr(weights), _stream(stream)), where)
+    _check(_lib().ra_write_weights(handle, int(seq), _ptr(weights),
+                                   _weights_stream(handle, stream)), where)
 
 
 def ra_export_weights(handle, seq, out, stream=None):
     where = "ra_export_weights"
     _arg(out, where, "out", torch.float32)
     _check(_lib().ra_export_weights(handle, int(seq), _ptr(out), 0 if out is None else out.numel(),
-                                    _stream(stream)), where)
+                                    _weights_stream(handle, stream)), where)
 
 
 def ra_write_positions(handle, seq, positions, stream=None):
@@ -680,7 +706,7 @@ class Cache:
         self.bounds = self.sparse_workspace = None       # (attach_sparse)
         self._sparse_streams = set()                     # handles they were used on
         self.weights = self.weights_workspace = None     # (attach_weights)
-        self._weight_streams = set()
+        self._weight_streams = set()                     # .. that the workspace was used on
         self.handle = ra_cache_create(cfg, self.k_pool, self.v_pool, self.pos_pool,
                                       pool_rows, self.meta, stream)
 
@@ -732,7 +758,7 @@ class Cache:
     def attach_weights(self, max_prompt_len, stream=None):
         """Accumulated weights, and the workspace of the steps that add to them, for prompts
         of up to max_prompt_len rows.  They are allocated for `stream`, and their memory is
-        kept until the steps made with them have ended, whatever streams these ran on."""
+        kept until the calls made with them have ended, whatever streams these ran on."""
         size = ra_weights_bytes(self.cfg, self.pool_rows)
         if size == 0:
             raise RandAttnError(RA_ERR_UNSUPPORTED, "ra_weights_bytes")
@@ -749,11 +775,9 @@ class Cache:
     def decode_biased(self, layer, rule, q, k_new, v_new, out, stream=None):
         workspace = self.workspace
         if self.weights is not None:
-            handle = _stream(stream)
+            stream = _stream(stream)
             workspace = self.weights_workspace
-            if handle not in self._weight_streams:
-                used_on = _torch_stream(handle, self.device)
-                self.weights.record_stream(used_on)
-                workspace.record_stream(used_on)
-                self._weight_streams.add(handle)
+            if stream not in self._weight_streams:
+                workspace.record_stream(_torch_stream(stream, self.device))
+                self._weight_streams.add(stream)
         ra_biased_attention(self.handle, layer, rule, q, k_new, v_new, out, workspace, stream)
