@@ -936,8 +936,9 @@ __global__ __launch_bounds__(NT) void move_weighed_kernel(
   __shared__ int src_of[kChunk];
   __shared__ int tbl[PAGED ? kMaxPagesLds : 1];
   __shared__ int s_chunk;
+  // the last heads first (see launch_weighed_moves)
   const int per_seq = L * Hkv;
-  const int head = static_cast<int>(blockIdx.x) / n_chunks;
+  const int head = static_cast<int>((gridDim.x - 1 - blockIdx.x) / n_chunks);
   const int slot = due.n ? due.slot[head / per_seq] : slot_lo + head / per_seq;
   const int lg = head % per_seq;
   const SeqMeta& M = meta[slot];
@@ -1231,6 +1232,10 @@ hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpoo
   // 63 and 36, 288 of 4,140 652 and 457), but not for many e4m3 heads (288 of 4,140 159 and 144,
   // 1,152 of 2,100 317 and 332, 2,304 of 4,140 1033 and 1116).  Rows have to move down by less
   // than a chunk: an event drops up to `every` rows, but under the external policy.
+  // The last heads move first: what wrote or read a request's rows before went from its first
+  // head to its last, as does what reads them next, and the last-level cache holds what was
+  // touched last (288 bf16 heads of 4,080 rows just written 209 us, from the first head on 240;
+  // their export afterwards 227 and 238).
   const int chunk = event_chunk_rows(sh.dtype);
   const int64_t n = (static_cast<int64_t>(max_candidates) + sh.r + 7 + chunk - 1) / chunk;
   const int64_t heads =

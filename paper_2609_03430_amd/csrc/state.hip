@@ -110,120 +110,167 @@ __global__ void append_positions_kernel(const SeqMeta* meta, int32_t* pos, int l
     pos[pool_row<PAGED>(rm, M.len + i)] = M.prompt_len + M.step + i;
 }
 
+// Value rows and value tiles hold the same elements in two orders: a thread takes four rows of
+// a row-major unit's kEpu channels, which are a quarter or a half of kEpu units of a tile.  The
+// tiles' side of the exchange is in LDS, so that global loads and stores are contiguous on
+// both sides.  Units there are permuted within runs of eight, since the units of a thread
+// and of its neighbours lie 128 bytes apart.
+__device__ __forceinline__ int lds_unit(int u) { return u ^ ((u >> 3) & 7); }
+template <typename E>
+using Four = E __attribute__((ext_vector_type(4)));
+// Rows that threads with four units each take.
+template <typename E>
+constexpr int copy_rows(int threads) {
+  return 4 * threads * 16 / (kHeadDim * static_cast<int>(sizeof(E)));
+}
+template <typename E>
+struct RowsOfTile {
+  static constexpr int kEpu = 16 / sizeof(E);
+  static constexpr int kUnitsRow = kHeadDim / kEpu;
+  // thread p's part of a workgroup's rows: r .. r + 3, channels ch .. ch + kEpu - 1
+  int r, ch;
+  __device__ __forceinline__ explicit RowsOfTile(int p)
+      : r(p / kUnitsRow * 4), ch(p % kUnitsRow * kEpu) {}
+  // .. the four rows of channel ch + c, in a tile's units in LDS
+  __device__ __forceinline__ Four<E>* at(u32x4* tiles, int c) const {
+    const int e = (r & ~7) * kHeadDim + (ch + c) * 8 + (r & 7);
+    return reinterpret_cast<Four<E>*>(tiles + lds_unit(e / kEpu)) + e % kEpu / 4;
+  }
+};
+
 // Row-major source rows [L*Hkv][len][128] into the cache layout of rows
 // [0, len) of each head; rows of a partly filled last value tile are
-// zeroed.  Grid: (ceil(len/64), L*Hkv).  A 64-row chunk may straddle two
-// pages of 32 rows, so rows are mapped one by one (value tiles of 8 rows
-// never straddle a page).
+// zeroed.  Grid: (ceil(len / copy_rows), L*Hkv).  A chunk of 64 rows may straddle
+// two pages of 32, so rows are mapped one by one (value tiles of 8 rows never
+// straddle a page).
+// Bound by HBM: 5.6 TB/s of reads and writes (288 bf16 heads of 4,096 rows 215 us; 64 of 2,048
+// 26).  The sources are read once, past the last-level cache, which is left to the rows
+// written; through the cache, with the values gathered from eight rows element by element,
+// these took 242 and 40 us.
+constexpr int kWriteThreads = 256;
 template <typename E, bool PAGED>
-__global__ void write_rows_kernel(SeqMeta M, int slot, int len, Paging pg,
-                                  const E* __restrict__ k_src,
-                                  const E* __restrict__ v_src,
-                                  const int32_t* __restrict__ pos_src,
-                                  E* __restrict__ kpool, E* __restrict__ vpool,
-                                  int32_t* __restrict__ pos) {
+__global__ __launch_bounds__(kWriteThreads) void write_rows_kernel(
+    SeqMeta M, int slot, int len, Paging pg, const E* __restrict__ k_src,
+    const E* __restrict__ v_src, const int32_t* __restrict__ pos_src, E* __restrict__ kpool,
+    E* __restrict__ vpool, int32_t* __restrict__ pos) {
   constexpr int kEpu = 16 / sizeof(E);
-  const int lg = blockIdx.y;
-  const int j0 = blockIdx.x * 64;
+  constexpr int kUnitsRow = kHeadDim / kEpu, kUnitsTile = 8 * kUnitsRow;
+  constexpr int kRows = copy_rows<E>(kWriteThreads);
+  __shared__ u32x4 tiles[4 * kWriteThreads];
+  const int lg = blockIdx.y, t = threadIdx.x;
+  const int j0 = blockIdx.x * kRows;
   const RowMap rm = row_map(M, slot, lg, pg);
-  const int64_t src0 = static_cast<int64_t>(lg) * len;
-  if (pos) {
-    for (int i = threadIdx.x; i < 64; i += blockDim.x) {
-      const int j = j0 + i;
-      if (j < len) pos[pool_row<PAGED>(rm, j)] = pos_src ? pos_src[src0 + j] : j;
-    }
-  }
+  const int64_t src0 = static_cast<int64_t>(lg) * len + j0;
+  const int n = min(kRows, len - j0);
+  if (pos && t < n) pos[pool_row<PAGED>(rm, j0 + t)] = pos_src ? pos_src[src0 + t] : j0 + t;
   if (!k_src) return;
-  constexpr int kUnitsRow = kHeadDim / kEpu;
-  for (int u = threadIdx.x; u < 64 * kUnitsRow; u += blockDim.x) {
-    const int j = j0 + u / kUnitsRow, col = u % kUnitsRow;
-    if (j < len)
-      *reinterpret_cast<u32x4*>(kpool + pool_row<PAGED>(rm, j) * kHeadDim + col * kEpu) =
-          *reinterpret_cast<const u32x4*>(k_src + (src0 + j) * kHeadDim + col * kEpu);
-  }
-  // values: each output 16-byte unit holds kEpu consecutive rows of one channel
-  constexpr int kUnitsCh = 8 / kEpu;
-  for (int u = threadIdx.x; u < 8 * kHeadDim * kUnitsCh; u += blockDim.x) {
-    const int tile = u / (kHeadDim * kUnitsCh);
-    const int rem = u % (kHeadDim * kUnitsCh);
-    const int ch = rem / kUnitsCh, part = rem % kUnitsCh;
-    const int jt = j0 + tile * 8;
-    if (jt >= len) continue;
-    E e[kEpu];
+  const u32x4* ks = reinterpret_cast<const u32x4*>(k_src + src0 * kHeadDim);
+  const u32x4* vs = reinterpret_cast<const u32x4*>(v_src + src0 * kHeadDim);
+  const RowsOfTile<E> part(t);
+  u32x4 k[4], v[4];
 #pragma unroll
-    for (int x = 0; x < kEpu; ++x) {
-      const int j = jt + part * kEpu + x;
-      e[x] = j < len ? v_src[(src0 + j) * kHeadDim + ch] : E(0);
-    }
-    u32x4 w;
-    __builtin_memcpy(&w, e, 16);
-    *reinterpret_cast<u32x4*>(vpool + pool_row<PAGED>(rm, jt) * kHeadDim + ch * 8 +
-                              part * kEpu) = w;
+  for (int i = 0; i < 4; ++i) {
+    const int u = t + i * kWriteThreads;
+    if (u < n * kUnitsRow) k[i] = __builtin_nontemporal_load(ks + u);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = u32x4{0u, 0u, 0u, 0u};
+    if (part.r + i < n)
+      v[i] = __builtin_nontemporal_load(vs + (part.r + i) * kUnitsRow + part.ch / kEpu);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int u = t + i * kWriteThreads;
+    if (u < n * kUnitsRow)
+      reinterpret_cast<u32x4*>(kpool + pool_row<PAGED>(rm, j0 + u / kUnitsRow) *
+                                           kHeadDim)[u % kUnitsRow] = k[i];
+  }
+  E in[4][kEpu];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) __builtin_memcpy(in[i], &v[i], 16);
+#pragma unroll
+  for (int c = 0; c < kEpu; ++c) {
+    const Four<E> four = {in[0][c], in[1][c], in[2][c], in[3][c]};
+    *part.at(tiles, c) = four;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int u = t + i * kWriteThreads, r = u / kUnitsTile * 8;
+    if (r < n)
+      reinterpret_cast<u32x4*>(vpool + pool_row<PAGED>(rm, j0 + r) * kHeadDim)[u % kUnitsTile] =
+          tiles[lds_unit(u)];
   }
 }
 
 // Rows [0, len) of heads lg, lg + 1, .. to row-major outputs [heads][len][128].
-// Grid: (ceil(len/32), 2, heads): keys, values; 128 threads.  One head is a short
-// copy (1.6 MB at 3,136 bf16 rows), so its time is the latency of a load and a
+// Grid: (ceil(len / copy_rows), 2, heads): keys, values; 128 threads.  One head is a
+// short copy (1.6 MB at 3,136 bf16 rows), so its time is the latency of a load and a
 // store: every thread issues all its loads before its stores, in 16-byte units
-// (outputs are 16-byte aligned, as all device pointers of the interface).  A thread takes kEpu channels x kEpu rows
-// of a value tile and transposes them in registers.  Element by element it
-// took 23 us per 3,136-row head, in 16-byte units 5.5, keys and values side by
-// side 4.5.
-constexpr int kReadRows = 32;
-template <typename E, bool PAGED>
-__global__ __launch_bounds__(128) void read_rows_kernel(SeqMeta M, int slot, int lg, int len,
-                                                        Paging pg, const E* __restrict__ kpool,
-                                                        const E* __restrict__ vpool,
-                                                        E* __restrict__ k_out,
-                                                        E* __restrict__ v_out) {
+// (outputs are 16-byte aligned, as all device pointers of the interface).  Element by
+// element it took 23 us per 3,136-row head, in 16-byte units 5.5, keys and values side by
+// side 4.5.  Many heads are bound by HBM, and read past the last-level cache, which the
+// outputs have: 64 bf16 heads of 2,048 rows 28 us, through the cache 41.  STREAM: outputs
+// of more than twice that cache go past it too (kStreamBytes).
+constexpr int kReadThreads = 128;
+template <typename E, bool PAGED, bool STREAM>
+__global__ __launch_bounds__(kReadThreads) void read_rows_kernel(
+    SeqMeta M, int slot, int lg, int len, Paging pg, const E* __restrict__ kpool,
+    const E* __restrict__ vpool, E* __restrict__ k_out, E* __restrict__ v_out) {
   constexpr int kEpu = 16 / sizeof(E);
   constexpr int kUnitsRow = kHeadDim / kEpu;
-  constexpr int kPer = kReadRows * kUnitsRow / 128;       // key units per thread
+  constexpr int kRows = copy_rows<E>(kReadThreads);
+  __shared__ u32x4 tiles[4 * kReadThreads];
+  const bool keys = blockIdx.y == 0;
+  E* out = keys ? k_out : v_out;
+  if (!out) return;
   const RowMap rm = row_map(M, slot, lg + blockIdx.z, pg);
-  const int64_t out0 = static_cast<int64_t>(blockIdx.z) * len;
-  const int j0 = blockIdx.x * kReadRows;                  // 32 rows lie in one page
-  const int64_t row0 = pool_row<PAGED>(rm, j0);
-  if (blockIdx.y == 0) {
-    if (!k_out) return;
-    u32x4 k[kPer];
-    const u32x4* src = reinterpret_cast<const u32x4*>(kpool + row0 * kHeadDim);
-    u32x4* dst = reinterpret_cast<u32x4*>(k_out + (out0 + j0) * kHeadDim);
-    const int n = min(kReadRows, len - j0) * kUnitsRow;
+  const int j0 = blockIdx.x * kRows, t = threadIdx.x;
+  const int n = min(kRows, len - j0);
+  // (the rows lie in one page, and so do the value tiles that hold the last of them)
+  const u32x4* src = reinterpret_cast<const u32x4*>((keys ? kpool : vpool) +
+                                                    pool_row<PAGED>(rm, j0) * kHeadDim);
+  u32x4* dst = reinterpret_cast<u32x4*>(
+      out + (static_cast<int64_t>(blockIdx.z) * len + j0) * kHeadDim);
+  const auto put = [&](int u, u32x4 x) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, dst + u);
+    else dst[u] = x;
+  };
+  const int units = (keys ? n : (n + 7) & ~7) * kUnitsRow;
+  u32x4 x[4];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int u = threadIdx.x + i * 128;
-      if (u < n) k[i] = src[u];
-    }
+  for (int i = 0; i < 4; ++i) {
+    const int u = t + i * kReadThreads;
+    if (u < units) x[i] = __builtin_nontemporal_load(src + u);
+  }
+  if (keys) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int u = threadIdx.x + i * 128;
-      if (u < n) dst[u] = k[i];
+    for (int i = 0; i < 4; ++i) {
+      const int u = t + i * kReadThreads;
+      if (u < units) put(u, x[i]);
     }
     return;
   }
-  if (!v_out) return;
-  for (int u = threadIdx.x; u < kReadRows / kEpu * kUnitsRow; u += 128) {
-    const int ch = u % kUnitsRow * kEpu, r = u / kUnitsRow * kEpu, j = j0 + r;
-    if (j >= len) continue;
-    // channel ch + c: rows r .. r + kEpu - 1 (of one 8-row tile)
-    E in[kEpu][kEpu];
-    const E* src = vpool + (row0 + (r & ~7)) * kHeadDim + ch * 8 + (r & 7);
 #pragma unroll
-    for (int c = 0; c < kEpu; ++c) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(src + c * 8);
-      __builtin_memcpy(in[c], &x, 16);
-    }
+  for (int i = 0; i < 4; ++i) {
+    const int u = t + i * kReadThreads;
+    if (u < units) tiles[lds_unit(u)] = x[i];
+  }
+  __syncthreads();
+  const RowsOfTile<E> part(t);
+  E rows[4][kEpu];
 #pragma unroll
-    for (int e = 0; e < kEpu; ++e) {
-      E out[kEpu];
+  for (int c = 0; c < kEpu; ++c) {
+    const Four<E> four = *part.at(tiles, c);
 #pragma unroll
-      for (int c = 0; c < kEpu; ++c) out[c] = in[c][e];
-      u32x4 x;
-      __builtin_memcpy(&x, out, 16);
-      if (j + e < len)
-        *reinterpret_cast<u32x4*>(v_out + (out0 + j + e) * kHeadDim + ch) = x;
-    }
+    for (int e = 0; e < 4; ++e) rows[e][c] = four[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    u32x4 w;
+    __builtin_memcpy(&w, rows[e], 16);
+    if (part.r + e < n) put((part.r + e) * kUnitsRow + part.ch / kEpu, w);
   }
 }
 
@@ -542,17 +589,11 @@ template <typename E>
 void write_rows_t(const Shape& sh, const SeqMeta& M, int slot, int len, const void* k_src,
                   const void* v_src, const int32_t* pos_src, void* kpool, void* vpool,
                   int32_t* pos, hipStream_t s) {
-  const dim3 grid((len + 63) / 64, sh.L * sh.Hkv);
-  const E* k = static_cast<const E*>(k_src);
-  const E* v = static_cast<const E*>(v_src);
-  if (sh.pg.tables)
-    hipLaunchKernelGGL((write_rows_kernel<E, true>), grid, dim3(256), 0, s, M, slot, len,
-                       sh.pg, k, v, pos_src, static_cast<E*>(kpool), static_cast<E*>(vpool),
-                       pos);
-  else
-    hipLaunchKernelGGL((write_rows_kernel<E, false>), grid, dim3(256), 0, s, M, slot, len,
-                       sh.pg, k, v, pos_src, static_cast<E*>(kpool), static_cast<E*>(vpool),
-                       pos);
+  const dim3 grid((len - 1) / copy_rows<E>(kWriteThreads) + 1, sh.L * sh.Hkv);
+  const auto kernel = sh.pg.tables ? write_rows_kernel<E, true> : write_rows_kernel<E, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kWriteThreads), 0, s, M, slot, len, sh.pg,
+                     static_cast<const E*>(k_src), static_cast<const E*>(v_src), pos_src,
+                     static_cast<E*>(kpool), static_cast<E*>(vpool), pos);
 }
 
 void write_rows_e4m3(const Shape& sh, const SeqMeta& M, int slot, int len, const void* k_src,
@@ -580,19 +621,25 @@ hipError_t launch_write_rows(const Shape& sh, const SeqMeta& M, int slot, int le
   return hipGetLastError();
 }
 
+// Keys and values from which outputs are stored past the last-level cache of 256 MB, which
+// else holds the last of them for whoever reads them next (microseconds with it and past it,
+// and of a sum over the outputs then: bf16, 168 MB 65 and 61, then 53 and 84; 302 MB 114 and
+// 104, then 108 and 128; 604 MB 213 and 201, then 210 and 207; fp32, 604 MB 226 and 215, then
+// 198 and 196; a request of 288 heads restored, evicted and saved again and again 764 and 718).
+constexpr int64_t kStreamBytes = int64_t(512) << 20;
 template <typename E>
 void read_rows_t(const Shape& sh, const SeqMeta& M, int slot, int lg, int heads, int len,
                  const void* kpool, const void* vpool, void* k_out, void* v_out,
                  hipStream_t s) {
-  const dim3 grid((len + kReadRows - 1) / kReadRows, 2, heads);
-  const E* k = static_cast<const E*>(kpool);
-  const E* v = static_cast<const E*>(vpool);
-  if (sh.pg.tables)
-    hipLaunchKernelGGL((read_rows_kernel<E, true>), grid, dim3(128), 0, s, M, slot, lg, len,
-                       sh.pg, k, v, static_cast<E*>(k_out), static_cast<E*>(v_out));
-  else
-    hipLaunchKernelGGL((read_rows_kernel<E, false>), grid, dim3(128), 0, s, M, slot, lg, len,
-                       sh.pg, k, v, static_cast<E*>(k_out), static_cast<E*>(v_out));
+  const dim3 grid((len - 1) / copy_rows<E>(kReadThreads) + 1, 2, heads);
+  const bool paged = sh.pg.tables;
+  const bool stream = int64_t(heads) * len * 2 * kHeadDim * int64_t(sizeof(E)) > kStreamBytes;
+  const auto kernel =
+      stream ? (paged ? read_rows_kernel<E, true, true> : read_rows_kernel<E, false, true>)
+             : (paged ? read_rows_kernel<E, true, false> : read_rows_kernel<E, false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(kReadThreads), 0, s, M, slot, lg, len, sh.pg,
+                     static_cast<const E*>(kpool), static_cast<const E*>(vpool),
+                     static_cast<E*>(k_out), static_cast<E*>(v_out));
 }
 
 // Heads lg .. lg + heads - 1 (at most 65,535 of them: a grid's z).
