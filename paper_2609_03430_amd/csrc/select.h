@@ -29,8 +29,8 @@ __device__ __forceinline__ int wave_inclusive_scan(int x) {
   return x;
 }
 
-template <int KEY_BITS>
-__device__ __forceinline__ int select_digit(int level, uint64_t key, uint32_t tie) {
+template <int KEY_BITS, typename Key>
+__device__ __forceinline__ int select_digit(int level, Key key, uint32_t tie) {
   constexpr int kKeyLevels = KEY_BITS / 8;
   if (level < kKeyLevels)
     return static_cast<int>((key >> (KEY_BITS - 8 - 8 * level)) & 0xFF);
@@ -39,9 +39,9 @@ __device__ __forceinline__ int select_digit(int level, uint64_t key, uint32_t ti
 
 // Returns this thread's drop mask (bit i: its candidate i is among the m
 // smallest (key, tie)).  `valid` marks the thread's real candidates.  All
-// threads of the block must call it.
-template <int NT, int KPT, int KEY_BITS>
-__device__ __forceinline__ uint32_t select_smallest(const uint64_t (&key)[KPT],
+// threads of the block must call it.  Keys of 32 bits may come as uint32_t, half the registers.
+template <int NT, int KPT, int KEY_BITS, typename Key>
+__device__ __forceinline__ uint32_t select_smallest(const Key (&key)[KPT],
                                                    const uint32_t (&tie)[KPT],
                                                    uint32_t valid, int m,
                                                    SelectShared& sh) {

@@ -65,8 +65,7 @@ __global__ __launch_bounds__(NT) void weight_event_kernel(const SeqMeta* __restr
     for (int i = t; i < n_pages; i += NT) tbl[i] = table[i];
     __syncthreads();
   }
-  uint64_t key[KPT];
-  uint32_t tie[KPT];
+  uint32_t key[KPT], tie[KPT];
   uint32_t valid = 0;
 #pragma unroll
   for (int i = 0; i < KPT; ++i) {
@@ -178,7 +177,9 @@ hipError_t launch_weight_event(const Shape& sh, const SeqMeta* meta, void* kpool
                                int32_t* pos, float* weights, int slot_lo, int slot_hi,
                                int max_candidates, bool positions_only, hipStream_t s) {
   if (slot_hi <= slot_lo) return hipSuccess;
-  // the smallest build that holds the candidates (as the random events')
+  // the smallest build that holds the candidates (as the random events'); the largest's keys
+  // are 32 bits for its registers' sake (2 heads of 17,000 and of 30,000 candidates 60 and
+  // 95 us, with keys of 64 bits, in scratch memory, 98 and 158; 64 of 30,000 110 and 168)
 #define RA_SELECT(KPT)                  \
   if (max_candidates <= 1024 * KPT)     \
   launch_select<1024, KPT>(sh, meta, pos, weights, slot_lo, slot_hi, s)
