@@ -965,7 +965,8 @@ ra_status ra_end_step(ra_cache* c, void* stream, int32_t* n_evicted) {
     for (int i = c->slot_lo; i < c->slot_hi; ++i) n_active += c->mirror[i].active;
     // (with block bounds attached a step may read part of the rows only: it moves none,
     // nor do steps of ra_biased_attention, the last of which expects the next one)
-    const bool defer = c->drops && !c->bounds && !c->weights && !c->biased_step && due == n_active && attention_plan(c).whole;
+    const bool defer = c->drops && !c->bounds && !c->weights && !c->biased_step &&
+                       due == n_active && attention_plan(c).whole;
     const int candidates = c->max_candidates_due();
     ra::DueList list;
     if (due <= ra::kDueList) {

@@ -230,7 +230,7 @@ ra_status ra_biased_attention(ra_cache* c, int32_t layer, const ra_score_rule* r
   a.waves = plan.launch_waves();
   a.arrivals = c->arrivals;
   ra::BiasLaunch b;
-  b.scale = rule->scale == 0.f ? 1.f / std::sqrt(static_cast<float>(ra::kHeadDim)) : rule->scale;
+  b.scale = rule->scale == 0.f ? 1.0 / std::sqrt(double(ra::kHeadDim)) : rule->scale;
   b.cap = rule->cap;
   b.slopes = rule->dev_slopes;
   b.window = rule->window;

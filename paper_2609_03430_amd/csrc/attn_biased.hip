@@ -57,12 +57,14 @@ struct BiasedSplits {
 constexpr int kNoWeights = 0, kWeighAfter = 1, kWeighHere = 2, kWeighBoth = 3;
 
 // The units of the scores; with KEEP each query's maximum and sum of a head.
-template <bool KEEP>
+template <bool KEEP, bool EXACT>
 struct RuleEnds {
   static constexpr bool kKeeps = KEEP;
-  float unit;
+  Unit unit;
   float* to;       // [G][2]
-  __device__ __forceinline__ float log2(float x) const { return x * unit; }
+  __device__ __forceinline__ float exp2(float x) const {
+    return EXACT ? exp2_exact(x, unit) : exp2f(x * unit.hi);
+  }
   __device__ __forceinline__ void keep(int q, float m, float l) const {
     to[2 * q] = m;
     to[2 * q + 1] = l;
@@ -123,16 +125,17 @@ __device__ __forceinline__ FourRows four_rows(const WindowBlocks& win, const Row
   const int j = (i < win.head ? i : i + win.shift) * kBlockRows + at % kBlockRows;
   return {j > len ? 0 : pool_row<PAGED>(rm, j), j};
 }
-template <typename Score4>
+template <bool EXACT, typename Score4>
 __device__ __forceinline__ void weigh_rows(f32x4* to, f32x4 w, int j, int len, int G,
-                                           const float* stats, float unit, Score4&& score4) {
+                                           const float* stats, Unit unit, Score4&& score4) {
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int q = 0; q < G; ++q) {
     const f32x4 x = score4(q);
     const float m = stats[2 * q], inv = 1.f / stats[2 * q + 1];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += exp2_fast((x[e] - m) * unit) * inv;
+    for (int e = 0; e < 4; ++e)
+      sum[e] += (EXACT ? exp2_exact(x[e] - m, unit) : exp2_fast((x[e] - m) * unit.hi)) * inv;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = j + e < len ? w[e] + sum[e] : j + e == len ? sum[e] : w[e];
@@ -148,6 +151,8 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
     int G, int Hq, int Hkv) {
   using E = typename R::Elem;
   using Two = typename R::New::Two;
+  constexpr bool kExact = std::is_same_v<R, F32Rows>;
+  const Unit unit{bias.unit, bias.unit_rest};
   __shared__ float s_m[W][kMaxGroup];
   __shared__ float s_l[W][kMaxGroup];
   __shared__ __align__(16) float s_o[W][kMaxGroup][kHeadDim];
@@ -267,7 +272,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
         store16(scores, at, x[0], x[1], x[2], x[3]);
         store16(scores, at + 16u, x[4], x[5], x[6], x[7]);
       }
-      R::attend(st, b.rows, x, bias.unit);
+      R::attend(st, b.rows, x, unit);
     };
     // two register buffers in turn; every prefetch is issued (the last block's again
     // once there is none left), so that the wait for a block leaves the next one's
@@ -304,7 +309,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
   const int first = static_cast<int>(threadIdx.x) * 4;
   FourRows rows{0, 0};
   f32x4 weights = {0.f, 0.f, 0.f, 0.f};
-  RuleEnds<WEIGH != kNoWeights> ends{bias.unit, nullptr};
+  RuleEnds<WEIGH != kNoWeights, kExact> ends{unit, nullptr};
   if constexpr (WEIGH == kWeighAfter)
     ends.to = bias.stats + 2 * (static_cast<int64_t>(w.slot) * Hq + w.g * G);
   if constexpr (kHere) {
@@ -325,11 +330,12 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
         const float* near =
             s_scores + kBlockRows * (owner * bias.lds_blocks + i - owner * per) + in_block;
         const float* from = far + static_cast<int64_t>(i) * G * kBlockRows + in_block;
-        weigh_rows(reinterpret_cast<f32x4*>(bias.weights + rows.row), weights, rows.j, w.len, G,
-                   &s_stats[0][0], bias.unit, [&](int q) {
-                     if (in_lds) return *reinterpret_cast<const f32x4*>(near + q * bias.lds_stride);
-                     return *reinterpret_cast<const f32x4*>(from + q * kBlockRows);
-                   });
+        weigh_rows<kExact>(
+            reinterpret_cast<f32x4*>(bias.weights + rows.row), weights, rows.j, w.len, G,
+            &s_stats[0][0], unit, [&](int q) {
+              if (in_lds) return *reinterpret_cast<const f32x4*>(near + q * bias.lds_stride);
+              return *reinterpret_cast<const f32x4*>(from + q * kBlockRows);
+            });
       }
       at += 4 * 64 * W;
       rows = four_rows<PAGED>(w.win, w.rm, w.len, at);
@@ -346,7 +352,7 @@ __global__ __launch_bounds__(64 * W, MINW) void attn_biased_kernel(
 // The weights of a launch whose scores went to the workspace.  Grid: (runs of 1,024 attended
 // rows, KV heads, slots), four rows to a thread.
 constexpr int kWeighThreads = 256, kWeighRows = 4;
-template <bool PAGED>
+template <bool PAGED, bool EXACT>
 __global__ __launch_bounds__(kWeighThreads) void add_weights_kernel(const SeqMeta* meta, int layer,
                                                                     BiasLaunch bias, Paging pg,
                                                                     int G, int Hq, int Hkv) {
@@ -362,9 +368,10 @@ __global__ __launch_bounds__(kWeighThreads) void add_weights_kernel(const SeqMet
   const float* s = bias.scores + head * bias.score_stride +
                    static_cast<int64_t>(at / kBlockRows) * G * kBlockRows + at % kBlockRows;
   f32x4* to = reinterpret_cast<f32x4*>(bias.weights + rows.row);
-  weigh_rows(to, *to, rows.j, len, G, bias.stats + 2 * head, bias.unit, [&](int q) {
-    return *reinterpret_cast<const f32x4*>(s + q * kBlockRows);
-  });
+  weigh_rows<EXACT>(to, *to, rows.j, len, G, bias.stats + 2 * head,
+                    Unit{bias.unit, bias.unit_rest}, [&](int q) {
+                      return *reinterpret_cast<const f32x4*>(s + q * kBlockRows);
+                    });
 }
 
 template <typename R, bool PAGED, bool BYPOS, int WEIGH>
@@ -373,7 +380,8 @@ void launch_biased(const Shape& sh, const AttnLaunch& a, const BiasLaunch& b, hi
   const SlotOrder order = sh.order ? *sh.order : SlotOrder{};
   const dim3 grid(a.max_splits, sh.Hkv, order.n ? order.n : a.max_seqs);
   hipLaunchKernelGGL((attn_biased_kernel<R, 4, kMinWaves, PAGED, BYPOS, WEIGH>), grid, dim3(256),
-                     WEIGH >= kWeighHere ? sh.G * b.lds_stride * sizeof(float) : 0, s, a, b, order, sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
+                     WEIGH >= kWeighHere ? sh.G * b.lds_stride * sizeof(float) : 0, s, a, b, order,
+                     sh.pg, sh.k_scale, sh.v_scale, sh.G, sh.Hq, sh.Hkv);
 }
 
 template <typename R, bool PAGED>
@@ -431,12 +439,12 @@ hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const B
   const int rows = a.max_splits * a.split_keys;
   const int per = kWeighThreads * kWeighRows;
   const dim3 grid((rows + per - 1) / per, sh.Hkv, a.max_seqs);
-  if (sh.pg.tables)
-    hipLaunchKernelGGL((add_weights_kernel<true>), grid, dim3(kWeighThreads), 0, s, a.meta, a.layer,
-                       b, sh.pg, sh.G, sh.Hq, sh.Hkv);
-  else
-    hipLaunchKernelGGL((add_weights_kernel<false>), grid, dim3(kWeighThreads), 0, s, a.meta,
-                       a.layer, b, sh.pg, sh.G, sh.Hq, sh.Hkv);
+  const bool paged = sh.pg.tables, exact = sh.dtype == 0;
+  const auto kernel =
+      paged ? (exact ? add_weights_kernel<true, true> : add_weights_kernel<true, false>)
+            : (exact ? add_weights_kernel<false, true> : add_weights_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(kWeighThreads), 0, s, a.meta, a.layer, b, sh.pg, sh.G,
+                     sh.Hq, sh.Hkv);
   return hipGetLastError();
 }
 

@@ -136,11 +136,11 @@ struct DenseSplits {
 // workgroup has more threads than the head has channel pairs, the splits are
 // dealt to `parts` groups of threads, which merge in LDS in split order.
 //
-// `ends` says what the maxima are in (log2(x): a difference of two in log2 units), and where
-// it keeps them is told the head's maximum and sum of each query.
+// `ends` says what the maxima are in (exp2(x): 2 to the difference x of two), and where it
+// keeps them is told the head's maximum and sum of each query.
 struct Log2Ends {
   static constexpr bool kKeeps = false;
-  __device__ __forceinline__ float log2(float x) const { return x; }
+  __device__ __forceinline__ float exp2(float x) const { return exp2f(x); }
   __device__ __forceinline__ void keep(int, float, float) const {}
 };
 template <typename E, int NT, typename Splits = DenseSplits, typename Ends = Log2Ends>
@@ -186,14 +186,14 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
       float mx = p.m;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) mx = fmaxf(mx, m[j]);
-      const float keep = exp2f(ends.log2(p.m - mx));
+      const float keep = ends.exp2(p.m - mx);
       p.m = mx;
       p.l *= keep;
       p.o0 *= keep;
       p.o1 *= keep;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const float w = s0 + j < hi ? exp2f(ends.log2(m[j] - mx)) : 0.f;
+        const float w = s0 + j < hi ? ends.exp2(m[j] - mx) : 0.f;
         p.l += w * l[j];
         p.o0 += w * x[j];
         p.o1 += w * y[j];
@@ -235,7 +235,7 @@ __device__ void merge_if_last(const AttnLaunch& a, int G, int Hq, int Hkv,
     for (int k = 1; k < parts && k * per < nsplit; ++k) {
       const Partial r = s_part[k * pairs + t];
       const float mx = fmaxf(p.m, r.m);
-      const float wp = exp2f(ends.log2(p.m - mx)), wr = exp2f(ends.log2(r.m - mx));
+      const float wp = ends.exp2(p.m - mx), wr = ends.exp2(r.m - mx);
       p = Partial{mx, p.l * wp + r.l * wr, p.o0 * wp + r.o0 * wr, p.o1 * wp + r.o1 * wr};
     }
     put(t, p);
@@ -389,7 +389,7 @@ __device__ __forceinline__ void finish_item(const AttnLaunch& a, const Work& w, 
     float lsum = 0.f, o = 0.f;
 #pragma unroll
     for (int v = 0; v < W; ++v) {
-      const float sc = exp2f(ends.log2(s_m[v][q] - mx));
+      const float sc = ends.exp2(s_m[v][q] - mx);
       lsum += s_l[v][q] * sc;
       o += s_o[v][q][c] * sc;
     }

@@ -27,6 +27,23 @@ __device__ __forceinline__ void staged_in_wave() {
 // 2^x, a result below 2^-126 flushed to zero: nothing beside a weight of 1.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// What turns a difference of two scores into log2 units: hi, and what its rounding left, which
+// fp32 rows take, too.
+struct Unit {
+  float hi, rest;
+};
+// 2^(x unit), of the product to 48 bits: its rounding to 24 would be an error of |x unit| 2^-24
+// of the result, more than those of the exponential itself from |x unit| = 2 on.
+__device__ __forceinline__ float exp2_exact(float x, Unit unit) {
+  const float y = x * unit.hi;
+  // (past fp32's range nothing is left, or infinity: any number will do beside an exponential
+  // of 0)
+  const float left =
+      __builtin_amdgcn_fmed3f(fmaf(x, unit.rest, fmaf(x, unit.hi, -y)), -1.f, 1.f);
+  const float e = exp2_fast(y);
+  return fmaf(e, left * 0.693147180559945309f, e);
+}
+
 // ---- bf16 rows -----------------------------------------------------------------
 
 struct Bf16Rows {
@@ -97,21 +114,22 @@ struct Bf16Rows {
   // compute_block in two: what is done to the scores stands between
   static __device__ __forceinline__ void scores(const Block& b, const Query& q, float (&x)[8]) {
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-  #pragma unroll
+#pragma unroll
     for (int s = 0; s < 4; ++s) {
       s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(b.k[0][s]), q.q[s], s0, 0, 0, 0);
       s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(b.k[1][s]), q.q[s], s1, 0, 0, 0);
     }
-  #pragma unroll
+#pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[i] = s0[i];
       x[4 + i] = s1[i];
     }
   }
   static __device__ __forceinline__ void attend(Softmax& st, const Block& b, const float (&x)[8],
-                                                float unit) {
+                                                Unit by) {
+    const float unit = by.hi;
     float bm = x[0];
-  #pragma unroll
+#pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
     const float mn = fmaxf(st.m, max_over_groups(bm));
     const float alpha = exp2_fast((st.m - mn) * unit);
@@ -119,7 +137,7 @@ struct Bf16Rows {
     // the bf16 MFMA (the remainder of a bf16 rounding is exact in fp32)
     bf16x8 p_hi, p_lo;
     float psum = 0.f;
-  #pragma unroll
+#pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float pf = exp2_fast((x[e] - mn) * unit);
       const __bf16 hi = static_cast<__bf16>(pf);
@@ -129,7 +147,7 @@ struct Bf16Rows {
     }
     st.l = st.l * alpha + psum;
     st.m = mn;
-  #pragma unroll
+#pragma unroll
     for (int u = 0; u < 8; ++u) {
       st.acc[u] *= alpha;
       st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(b.v[u]), p_hi, st.acc[u], 0, 0, 0);
@@ -329,7 +347,8 @@ struct E4m3Rows {
     }
   }
   static __device__ __forceinline__ void attend(Softmax& st, const Block& b, const float (&x)[8],
-                                                float unit) {
+                                                Unit by) {
+    const float unit = by.hi;
     float bm = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
@@ -365,16 +384,13 @@ struct E4m3Rows {
     scores(b, q, x);
     const int grp = (threadIdx.x & 63) >> 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-    x[i] *= scale_log2;
-    x[4 + i] *= scale_log2;
-  }
+    for (int e = 0; e < 8; ++e) x[e] *= scale_log2;
     if (limit < 32) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (8 * grp + e >= limit) x[e] = kNegInf;
     }
-    attend(st, b, x, 1.f);
+    attend(st, b, x, Unit{1.f, 0.f});
   }
   // The values of the keys whose bit is set in `hidden` (of the lane's eight) as zeros.
   static __device__ __forceinline__ void hide(Block& b, uint32_t hidden) {
@@ -489,45 +505,56 @@ struct F32Rows {
   static __device__ __forceinline__ float word(const u32x4& w, int i) {
     return __uint_as_float(w[i]);
   }
+  // Eight sums of 16 channels each, then theirs in pairs: a chain of all 128 rounds partial
+  // sums as large as the score 128 times, and left outputs and weights off by 1.6 to 3.6 times
+  // what torch's sums in fp32 do, these by 0.8 to 1.3 times.  Bound by the matrix cores and by
+  // latency (microseconds per layer, the chain and the eight sums: 16 heads of 200 rows 9.9 both,
+  // 8 of 2,200 15.3 and 15.9, 64 of 600 17.5 and 17.9, 256 of 900 41.7 and 42.8, of 4,000 176 and
+  // 177; with weights, 256 of 900 54.9 and 50.7).
   static __device__ __forceinline__ void scores(const Block& b, const Query& q, float (&x)[8]) {
-    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int t = 0; t < 2; ++t) {
+      f32x4 s[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int i = 0; i < 8; ++i) {
+        s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(word(b.k[t][i], e), q.q[i][e], s[t], 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+          s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(word(b.k[t][i], e), q.q[i][e], s[i], 0, 0, 0);
+      }
+      const f32x4 sum = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = s[0][i];
-      x[4 + i] = s[1][i];
+      for (int i = 0; i < 4; ++i) x[4 * t + i] = sum[i];
     }
   }
   static __device__ __forceinline__ void attend(Softmax& st, const Block& b, const float (&x)[8],
-                                                float unit) {
+                                                Unit unit) {
     float bm = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) bm = fmaxf(bm, x[e]);
     const float mn = fmaxf(st.m, max_over_groups(bm));
-    const float alpha = exp2_fast((st.m - mn) * unit);
+    const float alpha = exp2_fast((st.m - mn) * unit.hi);
     float p[8], psum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      p[e] = exp2_fast((x[e] - mn) * unit);
+      p[e] = exp2_exact(x[e] - mn, unit);
       psum += p[e];
     }
     st.l = st.l * alpha + psum;
     st.m = mn;
+    // product e takes key 8 * grp + e of each group of lanes; a block's sum is made by itself, so
+    // that the running one is rounded once a block
+    f32x4 sum[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) st.acc[u] *= alpha;
-    // product e takes key 8 * grp + e of each group of lanes
+    for (int u = 0; u < 8; ++u) sum[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        st.acc[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(word(b.v[u][e >> 2], e & 3), p[e],
-                                                         st.acc[u], 0, 0, 0);
+        sum[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(word(b.v[u][e >> 2], e & 3), p[e], sum[u], 0,
+                                                      0, 0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) st.acc[u] = st.acc[u] * alpha + sum[u];
   }
   static __device__ __forceinline__ void hide(Block& b, uint32_t hidden) {
 #pragma unroll

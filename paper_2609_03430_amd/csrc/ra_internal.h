@@ -309,7 +309,7 @@ hipError_t launch_block_attention(const Shape& sh, const AttnLaunch& a, const Bl
 // Attention whose scores follow a rule (attn_biased.hip): s = scale q.k, capped, less
 // slope * distance, and hidden past a window.
 struct BiasLaunch {
-  float scale = 0.f;
+  double scale = 0.0;
   float cap = 0.f;                // 0: none
   const float* slopes = nullptr;  // [Hq]
   int window = 0;                 // 0: none
@@ -318,6 +318,7 @@ struct BiasLaunch {
   // what the kernel keeps the scores in: a difference of two times `unit` is one in log2
   // units (see score_units)
   float unit = 1.f;
+  float unit_rest = 0.f;          // what unit's rounding left
   float before = 1.f;             // q.k times this: the cap's argument
   float after = 1.f;              // .. and the score times this: what is kept
   // accumulated weights (null: none kept), a float per pool row; the scores of the
@@ -332,15 +333,17 @@ struct BiasLaunch {
   int lds_blocks = 0;             // set by the launch: blocks of each wavefront whose scores
   int lds_stride = 0;             //   stay in LDS, and the floats a query takes there
 };
-// Scores stay as the products (or tanh of them) give them until a difference is taken, so
-// that no rounding of a score of 40 weighs in its exponential; slopes take them in natural
-// units first.
+// Scores stay as the products (or tanh of them) give them until a difference is taken, which
+// saves the rounding of each to log2 units, a relative error of its weight of up to 2^-24 of the
+// score; slopes take them in natural units first, with that rounding.
 inline void score_units(BiasLaunch& b) {
-  const float log2e = 1.4426950408889634f;
-  const float own = b.cap > 0.f ? b.cap : b.scale;
-  b.before = b.cap > 0.f ? b.scale / b.cap : 1.f;
-  b.after = b.slopes ? own : 1.f;
-  b.unit = b.slopes ? log2e : own * log2e;
+  const double log2e = 1.4426950408889634;
+  const double own = b.cap > 0.f ? double(b.cap) : b.scale;
+  const double unit = b.slopes ? log2e : own * log2e;
+  b.before = b.cap > 0.f ? static_cast<float>(b.scale / b.cap) : 1.f;
+  b.after = b.slopes ? static_cast<float>(own) : 1.f;
+  b.unit = static_cast<float>(unit);
+  b.unit_rest = static_cast<float>(unit - b.unit);
 }
 // Blocks that may hold rows within the window: `head` leading ones, then those from block
 // head + shift on.  Positions ascend, so a row within the window is one of the `window`
