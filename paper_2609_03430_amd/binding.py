@@ -90,10 +90,22 @@ class ra_rotary(ctypes.Structure):
         [(n, ctypes.c_int32) for n in ("dims", "pairs", "scaling", "original_len")]
 
 
+def _i32(x, where, name):
+    """An integer that the C interface takes as int32, which ctypes would wrap silently."""
+    n = int(x)
+    if n != x or not -2 ** 31 <= n < 2 ** 31:
+        raise RandAttnError(RA_ERR_INVALID_ARG, "%s (%s: %s, not an integer of 32 bits)"
+                            % (where, name, x))
+    return n
+
+
 def make_rotary(base, dims=128, pairs=RA_PAIRS_HALVES, scaling=RA_ROTARY_PLAIN, factor=1.0,
                 low=1.0, high=4.0, original_len=8192, magnitude=1.0):
     """factor, low, high and original_len apply to the scalings that read them."""
-    return ra_rotary(base, factor, low, high, magnitude, dims, pairs, scaling, original_len)
+    where = "make_rotary"
+    return ra_rotary(base, factor, low, high, magnitude, _i32(dims, where, "dims"),
+                     _i32(pairs, where, "pairs"), _i32(scaling, where, "scaling"),
+                     _i32(original_len, where, "original_len"))
 
 
 class ra_score_rule(ctypes.Structure):
@@ -105,7 +117,8 @@ class ra_score_rule(ctypes.Structure):
 def make_score_rule(scale=0.0, cap=0.0, slopes=None, window=0, prefix=0):
     """slopes: fp32 device tensor of a slope per query head, kept alive by the rule."""
     _arg(slopes, "make_score_rule", "slopes", torch.float32)
-    rule = ra_score_rule(scale, cap, _ptr(slopes), window, prefix)
+    rule = ra_score_rule(scale, cap, _ptr(slopes), _i32(window, "make_score_rule", "window"),
+                         _i32(prefix, "make_score_rule", "prefix"))
     rule.slopes = slopes
     return rule
 
@@ -590,6 +603,7 @@ def ra_rotate_rows(rotary, x, out, first=0, positions=None, stream=None):
     """Rows x [..., rows, 128] (fp32 or bf16) into `out`, which may be x; positions: int32,
     one per row of x."""
     where = "ra_rotate_rows"
+    first = _i32(first, where, "first")
     _arg(x, where, "x")
     if x is None or x.dtype not in (torch.float32, torch.bfloat16) or x.dim() < 2 or x.shape[-1] != 128:
         raise RandAttnError(RA_ERR_INVALID_ARG, where + " (x: not fp32 or bf16 rows of 128)")
@@ -602,18 +616,19 @@ def ra_rotate_rows(rotary, x, out, first=0, positions=None, stream=None):
     with torch.cuda.device(x.device):
         _check(_lib().ra_rotate_rows(ctypes.byref(rotary),
                                      RA_F32 if x.dtype == torch.float32 else RA_BF16, _ptr(x),
-                                     _ptr(out), n // rows if rows else 0, rows, int(first),
+                                     _ptr(out), n // rows if rows else 0, rows, first,
                                      _ptr(positions), _stream(stream)), where)
 
 
 def ra_biased_attention(handle, layer, rule, q, k_new, v_new, out, workspace, stream=None):
     where = "ra_biased_attention"
+    layer = _i32(layer, where, "layer")
     _decode_args(handle, where, q, k_new, v_new, out)
     cfg, slopes = _cfg_of(handle), getattr(rule, "slopes", None)
     if cfg is not None:
         _arg(slopes, where, "slopes", torch.float32, cfg.num_q_heads)
     _arg(workspace, where, "workspace")
-    _check(_lib().ra_biased_attention(handle, int(layer), ctypes.byref(rule), _ptr(q), _ptr(k_new),
+    _check(_lib().ra_biased_attention(handle, layer, ctypes.byref(rule), _ptr(q), _ptr(k_new),
                                       _ptr(v_new), _ptr(out), _ptr(workspace),
                                       0 if workspace is None else _bytes(workspace),
                                       _weights_stream(handle, stream)), where)
@@ -624,7 +639,8 @@ def ra_weights_bytes(cfg, pool_rows):
 
 
 def ra_weights_workspace_bytes(cfg, max_prompt_len):
-    return int(_lib().ra_weights_workspace_bytes(ctypes.byref(cfg), int(max_prompt_len)))
+    return int(_lib().ra_weights_workspace_bytes(
+        ctypes.byref(cfg), _i32(max_prompt_len, "ra_weights_workspace_bytes", "max_prompt_len")))
 
 
 def ra_weights_attach(handle, weights):
@@ -650,22 +666,25 @@ def _row_values(handle, seq):
 
 def ra_write_weights(handle, seq, weights, stream=None):
     where = "ra_write_weights"
+    seq = _i32(seq, where, "seq")
     _arg(weights, where, "weights", torch.float32, _row_values(handle, seq))
-    _check(_lib().ra_write_weights(handle, int(seq), _ptr(weights),
+    _check(_lib().ra_write_weights(handle, seq, _ptr(weights),
                                    _weights_stream(handle, stream)), where)
 
 
 def ra_export_weights(handle, seq, out, stream=None):
     where = "ra_export_weights"
+    seq = _i32(seq, where, "seq")
     _arg(out, where, "out", torch.float32)
-    _check(_lib().ra_export_weights(handle, int(seq), _ptr(out), 0 if out is None else out.numel(),
+    _check(_lib().ra_export_weights(handle, seq, _ptr(out), 0 if out is None else out.numel(),
                                     _weights_stream(handle, stream)), where)
 
 
 def ra_write_positions(handle, seq, positions, stream=None):
     where = "ra_write_positions"
+    seq = _i32(seq, where, "seq")
     _arg(positions, where, "positions", torch.int32, _row_values(handle, seq))
-    _check(_lib().ra_write_positions(handle, int(seq), _ptr(positions), _stream(stream)), where)
+    _check(_lib().ra_write_positions(handle, seq, _ptr(positions), _stream(stream)), where)
 
 
 def ra_attention_plan(handle):
