@@ -419,7 +419,7 @@ hipError_t launch_biased_attention(const Shape& sh, const AttnLaunch& a, const B
   // captured step, weights after and at once: bf16, 2 heads of 200 rows 9.6 and 7.8, 128 of 700
   // 18.2 and 16.0, 256 of 900 33.1 and 27.5, of 4,000 120 and 100, 512 of 1,100 73.0 and 64.7;
   // e4m3, 8 of 300 10.0 and 8.5, 256 of 200 13.3 and 10.9, of 7,400 119 and 104; fp32, 256 of
-  // 900 63.5 and 55.3); part of them, the rest through the workspace, gain less (256 of 9,216, G
+  // 900 65.2 and 56.0); part of them, the rest through the workspace, gain less (256 of 9,216, G
   // = 5, 260 and 234, of 12,000, G = 8, 357 and 348), and under half of 16 queries' nothing (160
   // e4m3 heads of 6,000 88 and 96)
   const bool alone = sh.dtype == 0 || b.heads <= 256;

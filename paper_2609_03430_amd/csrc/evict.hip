@@ -1234,8 +1234,8 @@ hipError_t launch_weighed_moves(const Shape& sh, const SeqMeta* meta, void* kpoo
   // than a chunk: an event drops up to `every` rows, but under the external policy.
   // The last heads move first: what wrote or read a request's rows before went from its first
   // head to its last, as does what reads them next, and the last-level cache holds what was
-  // touched last (288 bf16 heads of 4,080 rows just written 209 us, from the first head on 240;
-  // their export afterwards 227 and 238).
+  // touched last (288 bf16 heads of 4,080 rows just written 210 us, from the first head on 241;
+  // their export afterwards 212 and 216).
   const int chunk = event_chunk_rows(sh.dtype);
   const int64_t n = (static_cast<int64_t>(max_candidates) + sh.r + 7 + chunk - 1) / chunk;
   const int64_t heads =

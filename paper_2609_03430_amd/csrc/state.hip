@@ -144,9 +144,9 @@ struct RowsOfTile {
 // two pages of 32, so rows are mapped one by one (value tiles of 8 rows never
 // straddle a page).
 // Bound by HBM: 5.6 TB/s of reads and writes (288 bf16 heads of 4,096 rows 215 us; 64 of 2,048
-// 26).  The sources are read once, past the last-level cache, which is left to the rows
+// 27).  The sources are read once, past the last-level cache, which is left to the rows
 // written; through the cache, with the values gathered from eight rows element by element,
-// these took 242 and 40 us.
+// these took 242 and 40 us.  One head of 3,136 rows 6.2 us, call included (9.8).
 constexpr int kWriteThreads = 256;
 template <typename E, bool PAGED>
 __global__ __launch_bounds__(kWriteThreads) void write_rows_kernel(
@@ -167,28 +167,31 @@ __global__ __launch_bounds__(kWriteThreads) void write_rows_kernel(
   const u32x4* ks = reinterpret_cast<const u32x4*>(k_src + src0 * kHeadDim);
   const u32x4* vs = reinterpret_cast<const u32x4*>(v_src + src0 * kHeadDim);
   const RowsOfTile<E> part(t);
+  // (past the rows the last unit again: a load that lanes may branch around is waited for before
+  // the next one)
   u32x4 k[4], v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int u = t + i * kWriteThreads;
-    if (u < n * kUnitsRow) k[i] = __builtin_nontemporal_load(ks + u);
+    const int u = min(t + i * kWriteThreads, n * kUnitsRow - 1);
+    k[i] = __builtin_nontemporal_load(ks + u);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[i] = u32x4{0u, 0u, 0u, 0u};
-    if (part.r + i < n)
-      v[i] = __builtin_nontemporal_load(vs + (part.r + i) * kUnitsRow + part.ch / kEpu);
+    v[i] = __builtin_nontemporal_load(vs + min(part.r + i, n - 1) * kUnitsRow + part.ch / kEpu);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int u = t + i * kWriteThreads;
-    if (u < n * kUnitsRow)
-      reinterpret_cast<u32x4*>(kpool + pool_row<PAGED>(rm, j0 + u / kUnitsRow) *
-                                           kHeadDim)[u % kUnitsRow] = k[i];
+    const int u = min(t + i * kWriteThreads, n * kUnitsRow - 1);
+    reinterpret_cast<u32x4*>(kpool + pool_row<PAGED>(rm, j0 + u / kUnitsRow) *
+                                         kHeadDim)[u % kUnitsRow] = k[i];
   }
   E in[4][kEpu];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) __builtin_memcpy(in[i], &v[i], 16);
+  for (int i = 0; i < 4; ++i) {
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    const u32x4 row = part.r + i < n ? v[i] : zero;
+    __builtin_memcpy(in[i], &row, 16);
+  }
 #pragma unroll
   for (int c = 0; c < kEpu; ++c) {
     const Four<E> four = {in[0][c], in[1][c], in[2][c], in[3][c]};
@@ -205,26 +208,24 @@ __global__ __launch_bounds__(kWriteThreads) void write_rows_kernel(
 }
 
 // Rows [0, len) of heads lg, lg + 1, .. to row-major outputs [heads][len][128].
-// Grid: (ceil(len / copy_rows), 2, heads): keys, values; 128 threads.  One head is a
+// Grid: (ceil(len / copy_rows), sides, heads): keys (side 0), values; 128 threads.  One head is a
 // short copy (1.6 MB at 3,136 bf16 rows), so its time is the latency of a load and a
 // store: every thread issues all its loads before its stores, in 16-byte units
 // (outputs are 16-byte aligned, as all device pointers of the interface).  Element by
-// element it took 23 us per 3,136-row head, in 16-byte units 5.5, keys and values side by
-// side 4.5.  Many heads are bound by HBM, and read past the last-level cache, which the
-// outputs have: 64 bf16 heads of 2,048 rows 28 us, through the cache 41.  STREAM: outputs
+// element it took 23 us per 3,136-row head, in 16-byte units that wait for each other 4.5,
+// now 3.2.  Many heads are bound by HBM, and read past the last-level cache, which the
+// outputs have: 64 bf16 heads of 2,048 rows 26 us, through the cache 41.  STREAM: outputs
 // of more than twice that cache go past it too (kStreamBytes).
 constexpr int kReadThreads = 128;
 template <typename E, bool PAGED, bool STREAM>
 __global__ __launch_bounds__(kReadThreads) void read_rows_kernel(
     SeqMeta M, int slot, int lg, int len, Paging pg, const E* __restrict__ kpool,
-    const E* __restrict__ vpool, E* __restrict__ k_out, E* __restrict__ v_out) {
+    const E* __restrict__ vpool, E* __restrict__ k_out, E* __restrict__ v_out, int first_side) {
   constexpr int kEpu = 16 / sizeof(E);
   constexpr int kUnitsRow = kHeadDim / kEpu;
   constexpr int kRows = copy_rows<E>(kReadThreads);
   __shared__ u32x4 tiles[4 * kReadThreads];
-  const bool keys = blockIdx.y == 0;
-  E* out = keys ? k_out : v_out;
-  if (!out) return;
+  const bool keys = blockIdx.y + first_side == 0;
   const RowMap rm = row_map(M, slot, lg + blockIdx.z, pg);
   const int j0 = blockIdx.x * kRows, t = threadIdx.x;
   const int n = min(kRows, len - j0);
@@ -232,31 +233,24 @@ __global__ __launch_bounds__(kReadThreads) void read_rows_kernel(
   const u32x4* src = reinterpret_cast<const u32x4*>((keys ? kpool : vpool) +
                                                     pool_row<PAGED>(rm, j0) * kHeadDim);
   u32x4* dst = reinterpret_cast<u32x4*>(
-      out + (static_cast<int64_t>(blockIdx.z) * len + j0) * kHeadDim);
+      (keys ? k_out : v_out) + (static_cast<int64_t>(blockIdx.z) * len + j0) * kHeadDim);
   const auto put = [&](int u, u32x4 x) {
     if constexpr (STREAM) __builtin_nontemporal_store(x, dst + u);
     else dst[u] = x;
   };
   const int units = (keys ? n : (n + 7) & ~7) * kUnitsRow;
+  // (past the rows the last unit again: see write_rows_kernel)
   u32x4 x[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int u = t + i * kReadThreads;
-    if (u < units) x[i] = __builtin_nontemporal_load(src + u);
-  }
+  for (int i = 0; i < 4; ++i)
+    x[i] = __builtin_nontemporal_load(src + min(t + i * kReadThreads, units - 1));
   if (keys) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int u = t + i * kReadThreads;
-      if (u < units) put(u, x[i]);
-    }
+    for (int i = 0; i < 4; ++i) put(min(t + i * kReadThreads, units - 1), x[i]);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int u = t + i * kReadThreads;
-    if (u < units) tiles[lds_unit(u)] = x[i];
-  }
+  for (int i = 0; i < 4; ++i) tiles[lds_unit(t + i * kReadThreads)] = x[i];
   __syncthreads();
   const RowsOfTile<E> part(t);
   E rows[4][kEpu];
@@ -623,15 +617,16 @@ hipError_t launch_write_rows(const Shape& sh, const SeqMeta& M, int slot, int le
 
 // Keys and values from which outputs are stored past the last-level cache of 256 MB, which
 // else holds the last of them for whoever reads them next (microseconds with it and past it,
-// and of a sum over the outputs then: bf16, 168 MB 65 and 61, then 53 and 84; 302 MB 114 and
-// 104, then 108 and 128; 604 MB 213 and 201, then 210 and 207; fp32, 604 MB 226 and 215, then
-// 198 and 196; a request of 288 heads restored, evicted and saved again and again 764 and 718).
+// and of a sum over the outputs then: bf16, 168 MB 62 and 57, then 53 and 84; 302 MB 110 and 99,
+// then 108 and 128; 604 MB 214 and 201, then 210 and 208; fp32, 604 MB 226 and 214, then 200 and
+// 198; a request of 288 heads restored, evicted and saved again and again 751 and 710).
 constexpr int64_t kStreamBytes = int64_t(512) << 20;
 template <typename E>
 void read_rows_t(const Shape& sh, const SeqMeta& M, int slot, int lg, int heads, int len,
                  const void* kpool, const void* vpool, void* k_out, void* v_out,
                  hipStream_t s) {
-  const dim3 grid((len - 1) / copy_rows<E>(kReadThreads) + 1, 2, heads);
+  if (!k_out && !v_out) return;
+  const dim3 grid((len - 1) / copy_rows<E>(kReadThreads) + 1, k_out && v_out ? 2 : 1, heads);
   const bool paged = sh.pg.tables;
   const bool stream = int64_t(heads) * len * 2 * kHeadDim * int64_t(sizeof(E)) > kStreamBytes;
   const auto kernel =
@@ -639,7 +634,7 @@ void read_rows_t(const Shape& sh, const SeqMeta& M, int slot, int lg, int heads,
              : (paged ? read_rows_kernel<E, true, false> : read_rows_kernel<E, false, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(kReadThreads), 0, s, M, slot, lg, len, sh.pg,
                      static_cast<const E*>(kpool), static_cast<const E*>(vpool),
-                     static_cast<E*>(k_out), static_cast<E*>(v_out));
+                     static_cast<E*>(k_out), static_cast<E*>(v_out), k_out ? 0 : 1);
 }
 
 // Heads lg .. lg + heads - 1 (at most 65,535 of them: a grid's z).
