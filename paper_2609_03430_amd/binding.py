@@ -285,11 +285,10 @@ _WEIGHTS = {}
 def _weights_stream(handle, stream):
     """The raw stream of a call that uses the weights where any are attached."""
     raw = _stream(stream)
-    if _WEIGHTS:
-        weights, streams = _WEIGHTS.get(getattr(handle, "value", handle), (None, None))
-        if weights is not None and raw not in streams:
-            weights.record_stream(_torch_stream(raw, weights.device))
-            streams.add(raw)
+    weights, streams = _WEIGHTS.get(getattr(handle, "value", handle), (None, None))
+    if weights is not None and raw not in streams:
+        weights.record_stream(_torch_stream(raw, weights.device))
+        streams.add(raw)
     return raw
 
 
@@ -439,7 +438,8 @@ def ra_decode_attention_noalloc(handle, layer, q, k_new, v_new, out, stream=None
 
 def ra_end_step(handle, stream=None):
     n = ctypes.c_int32(0)
-    _check(_lib().ra_end_step(handle, _weights_stream(handle, stream), ctypes.byref(n)),
+    raw = _weights_stream(handle, stream) if _WEIGHTS else _stream(stream)
+    _check(_lib().ra_end_step(handle, raw, ctypes.byref(n)),
            "ra_end_step")
     return n.value
 
@@ -622,7 +622,9 @@ def ra_rotate_rows(rotary, x, out, first=0, positions=None, stream=None):
 
 def ra_biased_attention(handle, layer, rule, q, k_new, v_new, out, workspace, stream=None):
     where = "ra_biased_attention"
-    layer = _i32(layer, where, "layer")
+    layer = int(layer)
+    if layer >> 31:              # (here, as a call to check it costs as much as all other checks)
+        _i32(layer, where, "layer")
     _decode_args(handle, where, q, k_new, v_new, out)
     cfg, slopes = _cfg_of(handle), getattr(rule, "slopes", None)
     if cfg is not None:
@@ -631,7 +633,8 @@ def ra_biased_attention(handle, layer, rule, q, k_new, v_new, out, workspace, st
     _check(_lib().ra_biased_attention(handle, layer, ctypes.byref(rule), _ptr(q), _ptr(k_new),
                                       _ptr(v_new), _ptr(out), _ptr(workspace),
                                       0 if workspace is None else _bytes(workspace),
-                                      _weights_stream(handle, stream)), where)
+                                      _weights_stream(handle, stream) if _WEIGHTS
+                                      else _stream(stream)), where)
 
 
 def ra_weights_bytes(cfg, pool_rows):

