@@ -508,20 +508,20 @@ struct F32Rows {
   // Eight sums of 16 channels each, then theirs in pairs: a chain of all 128 rounds partial
   // sums as large as the score 128 times, and left outputs and weights off by 1.6 to 3.6 times
   // what torch's sums in fp32 do, these by 0.8 to 1.3 times.  Bound by the matrix cores and by
-  // latency (microseconds per layer, the chain and the eight sums: 16 heads of 200 rows 9.9 both,
-  // 8 of 2,200 15.3 and 15.9, 64 of 600 17.5 and 17.9, 256 of 900 41.7 and 42.8, of 4,000 176 and
-  // 177; with weights, 256 of 900 54.9 and 50.7).
+  // latency (microseconds per layer in a captured step, the chain and the eight sums: 2 heads of
+  // 200 rows 9.8 and 9.9, 8 of 600 13.6 and 13.9, of 2,200 16.9 and 17.4, 64 of 600 19.3 and 19.8,
+  // of 2,000 33.8 and 34.5, 256 of 900 51.6 and 52.5; of 4,000 the same).
   static __device__ __forceinline__ void scores(const Block& b, const Query& q, float (&x)[8]) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       f32x4 s[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 8; ++i) s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
           s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(word(b.k[t][i], e), q.q[i][e], s[i], 0, 0, 0);
-      }
       const f32x4 sum = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[4 * t + i] = sum[i];
