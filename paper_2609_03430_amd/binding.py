@@ -623,7 +623,7 @@ def ra_rotate_rows(rotary, x, out, first=0, positions=None, stream=None):
 def ra_biased_attention(handle, layer, rule, q, k_new, v_new, out, workspace, stream=None):
     where = "ra_biased_attention"
     layer = int(layer)
-    if layer >> 31:              # (here, as a call to check it costs as much as all other checks)
+    if layer >> 31:              # (checked inline: a call takes 0.3 us of the 2 of this one)
         _i32(layer, where, "layer")
     _decode_args(handle, where, q, k_new, v_new, out)
     cfg, slopes = _cfg_of(handle), getattr(rule, "slopes", None)

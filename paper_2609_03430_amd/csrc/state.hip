@@ -176,9 +176,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_rows_kernel(
     k[i] = __builtin_nontemporal_load(ks + u);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 4; ++i)
     v[i] = __builtin_nontemporal_load(vs + min(part.r + i, n - 1) * kUnitsRow + part.ch / kEpu);
-  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int u = min(t + i * kWriteThreads, n * kUnitsRow - 1);
@@ -208,7 +207,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_rows_kernel(
 }
 
 // Rows [0, len) of heads lg, lg + 1, .. to row-major outputs [heads][len][128].
-// Grid: (ceil(len / copy_rows), sides, heads): keys (side 0), values; 128 threads.  One head is a
+// Grid: (ceil(len / copy_rows), sides, heads): of keys (side 0) and values those that have an
+// output, so that no workgroup looks for one; 128 threads.  One head is a
 // short copy (1.6 MB at 3,136 bf16 rows), so its time is the latency of a load and a
 // store: every thread issues all its loads before its stores, in 16-byte units
 // (outputs are 16-byte aligned, as all device pointers of the interface).  Element by
